@@ -301,7 +301,7 @@ def _run_plain(st):
     scale = torch.where(valid, dlogp.reshape(-1)[seq].float(), 0.0)
     grad = -(ex / total)
     grad[rows, at] += 1.0
-    lse = top[:, 0].double() + logsum
+    lse = torch.where(valid, top[:, 0].double() + logsum, 0.0)
     return loss.float(), margin.float(), logp.float(), lse.float(), (grad * scale[:, None]).to(st["logits"].dtype)
 
 
@@ -366,10 +366,11 @@ def exact(case, seed):
     for i in range(2 * case["pairs"]):
         part = slice(first[i], first[i + 1])
         x, at = st["logits"][part].double(), st["targets"][part]
-        lse.append(torch.logsumexp(x, 1))
         lp = torch.log_softmax(x, 1)
         has = (at >= 0).nonzero()[:, 0]
-        token = torch.zeros_like(lse[-1])
+        token = torch.zeros_like(x[:, 0])
+        lse.append(torch.zeros_like(token))
+        lse[-1][has] = torch.logsumexp(x[has], 1)
         token[has] = lp[has, at[has]]
         logp.append(token)
         sums.append((token[has] - st["ref"][part][has].double()).sum())
@@ -410,4 +411,5 @@ def work(case):
         count = case["rows"] * case["d"]
         return dict(bytes=e * count * (3 if case["residual"] else 2), flops=count * (3 if case["residual"] else 2))
     t, v = case["tokens"], case["v"]
-    return dict(bytes=2 * e * t * v + 20 * t + 28 * case["pairs"], flops=t * v * 8)
+    # (the quarter of the tokens that carry no target is not read)
+    return dict(bytes=(e * t * v * 7) // 4 + 20 * t + 28 * case["pairs"], flops=t * v * 8)
