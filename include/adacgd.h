@@ -336,8 +336,99 @@ int adacgd_set_state(adacgd_ctx* ctx, int32_t field, const void* src, int64_t sr
 int adacgd_destroy(adacgd_ctx* ctx);
 
 /* Message of the last failure on this context, or, for ctx == NULL, of the
- * calling thread's last failed adacgd_init / adacgd_workspace_bytes. */
+ * calling thread's last failed adacgd_init / adacgd_workspace_bytes / operator below. */
 const char* adacgd_last_error(const adacgd_ctx* ctx);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * Operators of a model whose gradients the caller passes in (GRAD_EXTERNAL).  The engine wants the gradient of
+ * every worker at the same x; these are the layers of a model whose backward pass leaves them, each worker's (or
+ * each expert's) own, with a group of rows for each.
+ *
+ *  - Matrices are row-major with unit stride inside a row: element (r, c) of `t` is data[r * stride + c], of matrix g
+ *    of a grouped one data[g * group_stride + r * stride + c].  Rows may be any number of elements apart, so that a
+ *    gradient can be written to its place inside the engine's [n x d] array.  data needs the alignment of its type
+ *    only; rows that begin on 16 bytes are read and written faster.
+ *  - offsets is a DEVICE array of groups + 1 row numbers: group g owns rows [offsets[g], offsets[g+1]).  They must
+ *    ascend and lie in [0, rows]; equal ones leave a group empty.  The host does not read them.  Offsets that break
+ *    the rule give unspecified results, but nothing outside the matrices is read or written.  Rows before the first
+ *    and behind the last group are neither read nor written in any output that has a row for each of them.
+ *  - Sums are held in fp32 or fp64 and are formed in an order that depends on the sizes only: the same call gives the
+ *    same bits.
+ *  - Everything is enqueued on `stream` (a hipStream_t of the current device); no call allocates, synchronises or
+ *    keeps anything.  All of them may be captured into a graph.  A workspace is needed until the enqueued work has
+ *    completed and must not be shared by calls that may run at the same time; it need not be cleared.
+ *  - Outputs must not overlap inputs or each other, except where stated.
+ *  - Limits: rows below 2^31, at most 65535 groups, rows of at most 2^24 elements, strides below 2^31. */
+enum adacgd_dtype { ADACGD_FP32 = 0, ADACGD_BF16 = 1, ADACGD_FP16 = 2 };
+
+typedef struct {
+  void* data;           /* device                                                                         */
+  int32_t dtype;        /* adacgd_dtype                                                                   */
+  int32_t pad;          /* set to 0                                                                       */
+  int64_t stride;       /* elements from one row to the next, >= columns (not read where there is one row) */
+  int64_t group_stride; /* grouped matrices: elements from one matrix to the next; 0 = all groups share one
+                           (inputs only); otherwise not read                                              */
+} adacgd_tensor;
+
+/* Products of ragged groups of rows with a matrix for each group.
+ *   FORWARD  C[r] = B_g A[r]        A [rows x k], B [groups][n x k], C [rows x n]     (B_g: a layer's weights)
+ *   DX       C[r] = B_g^T A[r]      A [rows x n], B [groups][n x k], C [rows x k]
+ *   DW       C_g = sum_r A[r] B[r]^T over the rows of g: A [rows x n], B [rows x k], C [groups][n x k]; an empty
+ *            group's C_g is zero
+ * A and B have one type; C has that type or fp32.  Products are formed on the matrix cores (exactly, from bf16 and
+ * fp16) and summed in fp32; one rounding to C's type. */
+enum adacgd_product { ADACGD_FORWARD = 0, ADACGD_DX = 1, ADACGD_DW = 2 };
+
+/* Device bytes that the call of these sizes needs as workspace (0 for FORWARD and DX). */
+int adacgd_group_matmul_workspace_bytes(int32_t product, int32_t dtype, int64_t rows, int64_t groups, int64_t n, int64_t k,
+                                        int64_t* bytes);
+int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n, int64_t k, const int64_t* offsets,
+                        const adacgd_tensor* a, const adacgd_tensor* b, const adacgd_tensor* c, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* Layer normalisation of the rows of x [rows x d]: y = (x - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps),
+ * var the mean square of x - mean.  weight, bias: fp32 [d] or NULL (1 and 0).  mean, rstd: fp32 [rows], written; both
+ * NULL if no backward pass follows.  y has the type of x and may be x. */
+int adacgd_layer_norm(int64_t rows, int64_t d, const adacgd_tensor* x, const float* weight, const float* bias, double eps,
+                      const adacgd_tensor* y, float* mean, float* rstd, void* stream);
+
+/* Its gradients: dx for the rows of all groups, and for every group the gradients of weight and bias from its own rows,
+ * dweight, dbias: fp32 [groups x d] (an empty group's are zero), each may be NULL.  dy and dx have the type of x. */
+int adacgd_layer_norm_backward_workspace_bytes(int64_t rows, int64_t groups, int64_t d, int64_t* bytes);
+int adacgd_layer_norm_backward(int64_t rows, int64_t groups, int64_t d, const int64_t* offsets, const adacgd_tensor* dy,
+                               const adacgd_tensor* x, const float* weight, const float* mean, const float* rstd,
+                               const adacgd_tensor* dx, const adacgd_tensor* dweight, const adacgd_tensor* dbias,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
+/* out = residual + (kept ? x / (1 - p) : 0), element by element of x [rows x d].  Which elements are kept follows from
+ * (seed, step, layer, index) alone, so that no mask is stored: the backward pass is the same call on the gradient
+ * without the residual.  Element e = first + r d + c uses 16 bits of Philox4x32-10 with key = seed and counter
+ * (low word of e/8, high word of e/8, step, layer + 1): half (e % 2) of word (e % 8) / 2, low half first; it is kept
+ * if they are >= round(65536 p).  (The dither of the quantisers has 0 in the last word of its counter.)  1 / (1 - p) is
+ * taken of the rounded p; dropped elements count as 0 whatever x holds there, and with p = 1 all are dropped.
+ * step is the sum of `step` and, unless step_dev is NULL, of the device word *step_dev (modulo 2^32), so that replays
+ * of a captured call can draw anew.  residual may be NULL.  x, residual and out have one type; out may be x or residual. */
+int adacgd_dropout(int64_t rows, int64_t d, const adacgd_tensor* x, const adacgd_tensor* residual, const adacgd_tensor* out,
+                   double p, uint64_t seed, uint32_t step, const int64_t* step_dev, uint32_t layer, uint64_t first, void* stream);
+
+/* Preference loss of paired log ratios.  Sequence s owns the token rows [offsets[s], offsets[s+1]) of logits
+ * [tokens x v], s = 0 .. 2 pairs - 1; sequence 2p is the preferred one of pair p, 2p+1 the other.  With
+ * logp[t] = log softmax(logits[t])[targets[t]] and the same of a reference model given as ref,
+ *   margin[p] = sum over 2p of (logp - ref) - sum over 2p+1 of (logp - ref)
+ *   loss[p] = (1 - smoothing) log(1 + exp(-beta margin[p])) + smoothing log(1 + exp(beta margin[p])).
+ * Tokens whose target is outside [0, v) (prompts, padding) do not count: logp is 0 there and neither logits nor ref
+ * matter.  ref: fp32 [tokens], NULL for zeros.  loss, margin: fp32 [pairs]; logp and lse (log of the sum of
+ * exponentials, 0 at tokens that do not count): fp32 [tokens], all written.  Sums over tokens are held in fp64. */
+int adacgd_preference_loss_workspace_bytes(int64_t tokens, int64_t pairs, int64_t v, int64_t* bytes);
+int adacgd_preference_loss(int64_t tokens, int64_t pairs, int64_t v, const adacgd_tensor* logits, const int64_t* targets,
+                           const int64_t* offsets, const float* ref, double beta, double smoothing, float* loss,
+                           float* margin, float* logp, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* dlogits = sum_p dloss[p] d loss[p] / d logits, zero at tokens that do not count; dloss: fp32 [pairs].  dlogits has the
+ * type of logits and may be logits. */
+int adacgd_preference_loss_backward(int64_t tokens, int64_t pairs, int64_t v, const float* dloss, const adacgd_tensor* logits,
+                                    const int64_t* targets, const int64_t* offsets, const float* margin, const float* lse,
+                                    double beta, double smoothing, const adacgd_tensor* dlogits, void* stream);
 
 #ifdef __cplusplus
 }

@@ -14,6 +14,7 @@
 #include "../../include/adacgd.h"
 #include "devutil.h"
 #include "engine.h"
+#include "layers.h"
 #include "meeting.h"
 
 using namespace adacgd;
@@ -29,6 +30,18 @@ void set_err(char* buf, const char* fmt, ...) {
   vsnprintf(buf, 256, fmt, ap);
   va_end(ap);
 }
+
+}  // namespace
+
+int adacgd::fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+namespace {
 
 // bump allocator over the caller's workspace; with base == nullptr it only measures
 struct Carver {

@@ -1,0 +1,111 @@
+// What the operators of a model's layers share: element types, groups of rows, checks of arguments.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/adacgd.h"
+#include "devutil.h"
+
+namespace adacgd {
+
+// Sets the calling thread's last error and returns `code` (engine.hip).
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+constexpr int64_t kMaxCount = (int64_t(1) << 31) - 1;     // rows, groups, strides
+constexpr int64_t kMaxColumns = int64_t(1) << 24;
+
+inline int64_t dtype_size(int32_t t) { return t == ADACGD_FP32 ? 4 : 2; }
+
+// A matrix argument of `rows` rows (of each group, if it is a grouped one).
+inline int check_tensor(const adacgd_tensor* t, const char* name, int64_t rows, int64_t columns, bool grouped, bool may_share) {
+  if (!t) return fail(ADACGD_ERR_ARG, "%s is null", name);
+  if (t->dtype < 0 || t->dtype > ADACGD_FP16) return fail(ADACGD_ERR_ARG, "%s: unknown type %d", name, t->dtype);
+  if (t->pad != 0) return fail(ADACGD_ERR_ARG, "%s: pad must be 0", name);
+  if (rows > 0 && !t->data) return fail(ADACGD_ERR_ARG, "%s: data is null", name);
+  if ((uintptr_t)t->data % dtype_size(t->dtype)) return fail(ADACGD_ERR_ARG, "%s: data is not aligned to its type", name);
+  if (rows > 1 && (t->stride < columns || t->stride > kMaxCount))
+    return fail(ADACGD_ERR_ARG, "%s: stride must be in [%lld, 2^31), got %lld", name, (long long)columns, (long long)t->stride);
+  if (grouped && t->group_stride < 0) return fail(ADACGD_ERR_ARG, "%s: group_stride must not be negative", name);
+  if (grouped && !may_share && t->group_stride < (rows > 1 ? (rows - 1) * t->stride : 0) + columns)
+    return fail(ADACGD_ERR_ARG, "%s: group_stride is smaller than a matrix", name);
+  return ADACGD_OK;
+}
+inline int check_count(const char* name, int64_t v, int64_t lo, int64_t hi) {
+  if (v < lo || v > hi) return fail(ADACGD_ERR_ARG, "%s must be in [%lld, %lld], got %lld", name, (long long)lo, (long long)hi, (long long)v);
+  return ADACGD_OK;
+}
+inline int check_workspace(const void* w, int64_t have, int64_t need) {
+  if (need == 0) return ADACGD_OK;
+  if (!w || (uintptr_t)w % 256 || have < need)
+    return fail(ADACGD_ERR_ALLOC, "workspace of %lld bytes, 256-byte aligned, needed; %lld given", (long long)need, (long long)(w ? have : 0));
+  return ADACGD_OK;
+}
+// After a launch.
+inline int launched(const char* name) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? ADACGD_OK : fail(ADACGD_ERR_DEVICE, "%s: launch failed: %s", name, hipGetErrorString(e));
+}
+#define ADACGD_TRY(call)          \
+  do {                            \
+    const int rc_ = (call);       \
+    if (rc_) return rc_;          \
+  } while (0)
+
+// Rows are cut into slices of at most 2^SHIFT, none across two groups.  Slice j of group g has number
+// (offsets[g] >> SHIFT) + g + j: these numbers ascend without a prefix sum (a group of `len` rows that begins at o ends at
+// or below ((o + len) >> SHIFT) + 1), every group has one at least, and (rows >> shift) + groups bounds them, which is all
+// that the host knows.  Numbers that no slice has are left out by whoever gets them.
+// offsets are clamped where they are read, so that no value of theirs leads outside the matrices.
+struct Slice {
+  int64_t group;        // -1: none
+  int64_t begin, end;   // rows; empty only for an empty group
+  int64_t first, last;  // rows of the whole group
+};
+__host__ __device__ inline int64_t slice_numbers(int64_t rows, int64_t groups, int shift) { return (rows >> shift) + groups; }
+__device__ __forceinline__ int64_t offset_at(const int64_t* offsets, int64_t i, int64_t rows) {
+  const int64_t o = offsets[i];
+  return o < 0 ? 0 : o > rows ? rows : o;
+}
+// All lanes of a wavefront call it with the same arguments: 64 groups are looked at with one load.  `each` entries of
+// offsets make one group.
+__device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t groups, int64_t rows, int64_t each, int shift, int64_t number) {
+  Slice s{-1, 0, 0, 0, 0};
+  int64_t low = 0, count = groups;
+  const int lane = (int)lane_id();
+  for (;;) {
+    const int64_t step = (count + 63) / 64;
+    const bool here = lane * step < count;
+    const int64_t g = low + (here ? lane * step : 0);
+    const uint64_t m = ballot(here && (offset_at(offsets, g * each, rows) >> shift) + g <= number);
+    if (m == 0) return s;
+    const int64_t hit = 63 - __builtin_clzll(m);          // (the last of them)
+    low += hit * step;
+    count = count - hit * step < step ? count - hit * step : step;
+    if (step == 1) break;
+  }
+  s.first = offset_at(offsets, low * each, rows);
+  s.last = offset_at(offsets, (low + 1) * each, rows);
+  if (s.last < s.first) s.last = s.first;
+  const int64_t j = number - ((s.first >> shift) + low);
+  s.begin = s.first + (j << shift);
+  if (s.begin >= s.last && j > 0) return s;
+  s.group = low;
+  s.end = s.begin + (int64_t(1) << shift) < s.last ? s.begin + (int64_t(1) << shift) : s.last;
+  return s;
+}
+
+// Element types: what is stored, and its value as a float.
+template <typename T>
+__device__ __forceinline__ float to_float(T v) { return (float)v; }
+template <typename T>
+__device__ __forceinline__ T from_float(float v) { return (T)v; }      // (to nearest, ties to even)
+
+// f(type tag) for the C type of a dtype.
+template <typename F>
+inline int by_dtype(int32_t dtype, F f) {
+  if (dtype == ADACGD_FP32) return f(float());
+  if (dtype == ADACGD_BF16) return f(__bf16());
+  return f(_Float16());
+}
+
+}  // namespace adacgd

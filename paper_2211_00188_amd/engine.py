@@ -33,7 +33,11 @@ KERNELS = ["xupdate", "grad_margin", "grad_cols", "aggregate",
            "w_rank", "m_rank", "w_eig", "m_eig"]
 
 EXPORTS = ["adacgd_workspace_bytes", "adacgd_init", "adacgd_init_static", "adacgd_step", "adacgd_state", "adacgd_set_state",
-           "adacgd_destroy", "adacgd_last_error"]
+           "adacgd_destroy", "adacgd_last_error",
+           # operators of a model's layers (bound in layers.py)
+           "adacgd_group_matmul_workspace_bytes", "adacgd_group_matmul", "adacgd_layer_norm",
+           "adacgd_layer_norm_backward_workspace_bytes", "adacgd_layer_norm_backward", "adacgd_dropout",
+           "adacgd_preference_loss_workspace_bytes", "adacgd_preference_loss", "adacgd_preference_loss_backward"]
 
 
 class Level(C.Structure):

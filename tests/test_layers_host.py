@@ -1,0 +1,142 @@
+"""Operators of a model's layers, what can be checked without a GPU: refusals of the C entry points and of the binding,
+sizes of workspaces, and the arithmetic by which ragged groups are cut into slices."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+
+from paper_2211_00188_amd import engine as E
+from paper_2211_00188_amd import layers as L
+
+pytestmark = pytest.mark.skipif(not os.path.exists(E.LIB_PATH), reason="libadacgd.so not built")
+
+P = 4096          # an address that is aligned and that no refused call reads
+ARG, ALLOC = 1, 3
+
+
+def T(data=P, dtype=0, stride=64, group_stride=0, pad=0):
+    return C.byref(L.Tensor(data, dtype, pad, stride, group_stride))
+
+
+def refused(name, args, code=ARG, text=""):
+    lib = L._library()
+    assert getattr(lib, name)(*args) == code, lib.adacgd_last_error(None)
+    message = lib.adacgd_last_error(None).decode()
+    assert text in message and message, message
+
+
+def test_every_entry_point_is_bound():
+    assert set(L.ARGTYPES) <= set(E.EXPORTS)
+
+
+GOOD = dict(product=0, rows=10, groups=2, n=64, k=32, offsets=P, a=T(), b=T(group_stride=4096), c=T(), ws=None, size=0, stream=None)
+
+
+@pytest.mark.parametrize("bad,code,text", [
+    (dict(product=3), ARG, "product"), (dict(product=-1), ARG, "product"), (dict(rows=-1), ARG, "rows"), (dict(rows=1 << 31), ARG, "rows"),
+    (dict(groups=0), ARG, "groups"), (dict(groups=1 << 31), ARG, "groups"), (dict(n=0), ARG, "n must"), (dict(k=0), ARG, "k must"),
+    (dict(n=(1 << 24) + 1), ARG, "n must"), (dict(offsets=None), ARG, "offsets"), (dict(a=None), ARG, "a is null"),
+    (dict(a=T(data=None)), ARG, "a: data"), (dict(a=T(dtype=3)), ARG, "type"), (dict(a=T(dtype=-1)), ARG, "type"), (dict(a=T(pad=1)), ARG, "pad"),
+    (dict(a=T(data=P + 2)), ARG, "aligned"), (dict(a=T(stride=31)), ARG, "stride"), (dict(a=T(stride=1 << 31)), ARG, "stride"),
+    (dict(b=T(group_stride=-64)), ARG, "group_stride"), (dict(b=T(dtype=1)), ARG, "differ in type"), (dict(c=T(dtype=1)), ARG, "c has neither"),
+    (dict(c=T(stride=63)), ARG, "stride"),
+    (dict(product=2, c=T(stride=64, group_stride=63 * 64)), ARG, "smaller than a matrix"), (dict(product=2, c=T(group_stride=0)), ARG, "smaller"),
+])
+def test_bad_products_are_refused(bad, code, text):
+    refused("adacgd_group_matmul", list(dict(GOOD, **bad).values()), code, text)
+
+
+def test_products_without_rows_need_no_data():
+    lib = L._library()
+    for product in (0, 1):
+        args = dict(GOOD, product=product, rows=0, a=T(data=None), c=T(data=None))
+        assert lib.adacgd_group_matmul(*args.values()) == 0, lib.adacgd_last_error(None)
+
+
+def test_workspace_of_the_products():
+    lib, n = L._library(), C.c_int64(-1)
+    for product in (0, 1):
+        assert lib.adacgd_group_matmul_workspace_bytes(product, 1, 100000, 7, 512, 512, C.byref(n)) == 0 and n.value == 0
+    assert lib.adacgd_group_matmul_workspace_bytes(2, 1, 100000, 7, 512, 512, C.byref(n)) == 0 and n.value >= 0 and n.value % 256 == 0
+    refused("adacgd_group_matmul_workspace_bytes", [0, 0, 1, 1, 1, 1, None], ARG, "bytes")
+    refused("adacgd_group_matmul_workspace_bytes", [0, 5, 1, 1, 1, 1, C.byref(n)], ARG, "type")
+    refused("adacgd_group_matmul_workspace_bytes", [4, 0, 1, 1, 1, 1, C.byref(n)], ARG, "product")
+
+
+NORM = dict(rows=10, d=64, x=T(), weight=None, bias=None, eps=1e-5, y=T(), mean=None, rstd=None, stream=None)
+
+
+@pytest.mark.parametrize("bad,text", [
+    (dict(rows=-1), "rows"), (dict(d=0), "d must"), (dict(d=1 << 25), "d must"), (dict(x=None), "x is null"), (dict(y=T(dtype=1)), "differ in type"),
+    (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(mean=P), "together"), (dict(rstd=P), "together"),
+    (dict(x=T(stride=10)), "stride"), (dict(y=T(data=P + 1)), "aligned"),
+])
+def test_bad_norms_are_refused(bad, text):
+    refused("adacgd_layer_norm", list(dict(NORM, **bad).values()), ARG, text)
+
+
+BACK = dict(rows=10, groups=2, d=64, offsets=P, dy=T(), x=T(), weight=None, mean=P, rstd=P, dx=T(), dw=T(), db=T(), ws=None, size=0, stream=None)
+
+
+@pytest.mark.parametrize("bad,text", [
+    (dict(groups=0), "groups"), (dict(offsets=None), "offsets"), (dict(dy=T(dtype=1)), "differ in type"), (dict(dx=T(dtype=2)), "differ in type"),
+    (dict(mean=None), "mean or rstd"), (dict(rstd=None), "mean or rstd"), (dict(dw=T(dtype=1)), "fp32"), (dict(db=T(stride=63)), "dbias: stride"),
+    (dict(dw=T(data=None)), "dweight: data"),
+])
+def test_bad_norm_gradients_are_refused(bad, text):
+    refused("adacgd_layer_norm_backward", list(dict(BACK, **bad).values()), ARG, text)
+
+
+DROP = dict(rows=10, d=64, x=T(), residual=None, out=T(), p=0.5, seed=1, step=0, step_dev=None, layer=0, first=0, stream=None)
+
+
+@pytest.mark.parametrize("bad,text", [
+    (dict(p=-0.01), "p must"), (dict(p=1.01), "p must"), (dict(p=float("nan")), "p must"), (dict(layer=0xFFFFFFFF), "layer"),
+    (dict(residual=T(dtype=1)), "differ in type"), (dict(out=T(dtype=1)), "differ in type"), (dict(out=None), "out is null"),
+    (dict(residual=T(stride=3)), "residual: stride"),
+])
+def test_bad_dropout_is_refused(bad, text):
+    refused("adacgd_dropout", list(dict(DROP, **bad).values()), ARG, text)
+
+
+LOSS = dict(tokens=10, pairs=2, v=64, logits=T(), targets=P, offsets=P, ref=None, beta=0.1, smoothing=0.0, loss=P, margin=P, logp=P, lse=P,
+            ws=P, size=1 << 40, stream=None)
+GRAD = dict(tokens=10, pairs=2, v=64, dloss=P, logits=T(), targets=P, offsets=P, margin=P, lse=P, beta=0.1, smoothing=0.0, out=T(), stream=None)
+SHARED = [(dict(tokens=-1), "tokens"), (dict(pairs=-1), "pairs"), (dict(v=0), "v must"), (dict(targets=None), "targets"), (dict(offsets=None), "offsets"),
+          (dict(beta=float("nan")), "beta"), (dict(beta=float("inf")), "beta"), (dict(smoothing=-0.1), "smoothing"), (dict(smoothing=1.5), "smoothing"),
+          (dict(smoothing=float("nan")), "smoothing"), (dict(logits=T(stride=8)), "stride")]
+
+
+@pytest.mark.parametrize("bad,text", SHARED + [(dict(loss=None), "loss"), (dict(margin=None), "margin"), (dict(logp=None), "logp"), (dict(lse=None), "lse")])
+def test_bad_preference_losses_are_refused(bad, text):
+    refused("adacgd_preference_loss", list(dict(LOSS, **bad).values()), ARG, text)
+
+
+@pytest.mark.parametrize("bad,text", SHARED + [(dict(dloss=None), "dloss"), (dict(margin=None), "margin"), (dict(lse=None), "lse"),
+                                               (dict(out=T(dtype=1)), "differ in type")])
+def test_bad_preference_gradients_are_refused(bad, text):
+    refused("adacgd_preference_loss_backward", list(dict(GRAD, **bad).values()), ARG, text)
+
+
+def test_the_binding_refuses_host_tensors():
+    import torch
+    x, off = torch.zeros(4, 8), torch.tensor([0, 4])
+    for call in (lambda: L.group_matmul(x, x[None], off), lambda: L.group_matmul_dw(x, x, off), lambda: L.layer_norm(x),
+                 lambda: L.dropout(x, 0.5, 1), lambda: L.preference_loss(x, off, off)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
+
+
+@pytest.mark.parametrize("shift", [4, 5, 6, 7, 8, 13])
+def test_numbers_of_slices_ascend_without_a_prefix_sum(shift):
+    """(offset >> shift) + group + j: ascending, one at least for every group, below (rows >> shift) + groups."""
+    rng = np.random.default_rng(shift)
+    for trial in range(200):
+        groups = int(rng.integers(1, 40))
+        sizes = rng.integers(0, 4 << shift, groups) * (rng.random(groups) < 0.8)
+        first = int(rng.integers(0, 3 << shift))
+        o = np.concatenate([[first], first + np.cumsum(sizes)])
+        rows = int(o[-1] + rng.integers(0, 2 << shift))
+        numbers = [(int(o[g]) >> shift) + g + j for g in range(groups) for j in range(max(1, -(-int(sizes[g]) >> shift)))]
+        assert all(a < b for a, b in zip(numbers, numbers[1:])) and numbers[-1] < (rows >> shift) + groups
