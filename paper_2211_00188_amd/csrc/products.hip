@@ -1,66 +1,314 @@
-// Matrix products of ragged groups of rows: C[r] = B_g A[r], its transpose, and the sum of the outer products of a group.
+// Matrix products of ragged groups of rows, on the matrix cores: C[r] = B_g A[r], its transpose, and the sum of the outer
+// products of a group.
+//
+// All three are C(m, n) = sum_r A(m, r) B(n, r).  An operand either has the summed index r contiguous in memory ("along")
+// or the other one ("across"): FORWARD has both along, DX has B across, DW both.  A block forms a tile of C; slabs of both
+// operands, 128 bytes of r wide (64 elements of 16 bits, 32 of fp32), go through LDS, two of them: one is loaded while the
+// other is multiplied.
+//   along:   R rows of 128 bytes.  Lanes of a fragment read 16 bytes of 16 rows; the 16-byte chunk c of row r is kept at
+//            c ^ (r & 7), so that eight rows lie in different banks.
+//   across:  a row of R elements for each r.  16-bit fragments are read transposed (ds_read_b64_tr_b16: 16 lanes take four
+//            rows of 16 elements and get four rows' values of one column each), fp32 ones element by element.  Pieces of 16
+//            elements are kept at piece ^ (a function of the row) so that the rows read together lie in different banks.
+// Matrix instructions get B as first operand: a lane then holds four neighbouring columns of a row of C.
+// The order of the summed index inside an instruction does not matter as long as both operands agree on it: lane group q
+// (lane / 16) holds the q-th 16 bytes of a row's 64, eight elements of one instruction, or one element of each of four in fp32.
 #include "layers.h"
 
 namespace adacgd {
 namespace {
 
-constexpr int kTileShift = 6, kTileRows = 1 << kTileShift;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kSlab = 128;      // bytes of the summed index
 
 struct ProductArgs {
   const void* a;
   const void* b;
   void* c;
+  float* partial;                       // DW: slices' sums, where groups are cut
   const int64_t* offsets;
   int64_t rows, groups, each;           // `each` entries of offsets to a group
   int64_t lda, ldb, ldc, gsb, gsc;
-  int n, k;
+  int64_t slices;                       // numbers of slices
+  int n, k, shift;
 };
 
-// C tile of 64 x 64 from A(m, r) and B(n, r) summed over r, any layout: element (m, r) of A is at m am + r ar.
-template <typename T, typename O>
-__device__ void tile_product(const T* a, int64_t am, int64_t ar, int m, const T* b, int64_t bn, int64_t br, int n, int64_t red,
-                             O* c, int64_t cm) {
-  __shared__ float As[16][64 + 1], Bs[16][64 + 1];
-  const int t = threadIdx.x, tx = t % 16, ty = t / 16;
-  float acc[4][4] = {};
-  for (int64_t r0 = 0; r0 < red; r0 += 16) {
-    for (int i = t; i < 16 * 64; i += 256) {
-      const int r = i % 16, q = i / 16;
-      const bool in = r0 + r < red;
-      As[r][q] = in && q < m ? to_float(a[q * am + (r0 + r) * ar]) : 0.f;
-      Bs[r][q] = in && q < n ? to_float(b[q * bn + (r0 + r) * br]) : 0.f;
-    }
-    __syncthreads();
-    for (int r = 0; r < 16; ++r)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(As[r][ty * 4 + i], Bs[r][tx * 4 + j], acc[i][j]);
-    __syncthreads();
+// One operand of a tile: `valid` of the tile's rows (along) or columns (across) exist.
+struct Operand {
+  const char* p;
+  int64_t pitch;        // bytes from one row of memory to the next
+  int valid;
+};
+
+__device__ __forceinline__ f32x4 multiply(float, word4 b, word4 a, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[j]), __uint_as_float(a[j]), c, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ f32x4 multiply(__bf16, word4 b, word4 a, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(_Float16, word4 b, word4 a, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+}
+
+// Slabs of one operand: R rows or columns of the tile, W wavefronts load it.
+template <typename T, bool ACROSS, int R, int W>
+struct Loader {
+  static constexpr int kElem = 16 / sizeof(T);                            // elements of a chunk
+  static constexpr int kDepth = kSlab / sizeof(T);                        // summed indexes of a slab
+  static constexpr int kRow = ACROSS ? R * (int)sizeof(T) : kSlab;        // bytes of a row in LDS
+  static constexpr int kLoads = R * kSlab / 1024 / W;                     // of 16 bytes a lane
+  static constexpr int kBytes = R * kSlab;
+  static_assert(kLoads * 1024 * W == kBytes, "");
+
+  // where pieces of row `k` are put, in chunks
+  static __device__ __forceinline__ int turn(int k) {
+    if (!ACROSS) return k & 7;
+    return sizeof(T) == 2 ? ((k & 3) + ((k >> 3 & 1) << 2)) << 1 : (k >> 2 & 3) << 2;
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j)
-      if (ty * 4 + i < m && tx * 4 + j < n) c[(ty * 4 + i) * cm + tx * 4 + j] = from_float<O>(acc[i][j]);
-}
+  // row in LDS and chunk of that row's memory that the lane's i-th 16 bytes hold
+  static __device__ __forceinline__ void place(int wave, int lane, int i, int& row, int& chunk) {
+    const int at = (i * W + wave) * 1024 + lane * 16;
+    row = at / kRow;
+    chunk = at % kRow / 16 ^ turn(row);
+  }
 
-template <typename T, typename O, bool TRANSPOSED>
-__global__ void __launch_bounds__(256) k_rows_product(ProductArgs p) {
-  const Slice s = find_slice(p.offsets, p.groups, p.rows, p.each, kTileShift, blockIdx.y);
+  uint32_t off[kLoads];
+  __device__ __forceinline__ void init(const Operand& o, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row, chunk;
+      place(wave, lane, i, row, chunk);
+      off[i] = (uint32_t)(row * o.pitch) + chunk * 16;
+    }
+  }
+  // Straight into LDS: rows begin on 16 bytes and are whole chunks.  What lies behind the operand reads as zero.
+  __device__ __forceinline__ void direct(const Operand& o, int64_t red, int64_t r0, char* lds, int wave, int lane) const {
+    const int64_t left = red - r0;
+    if constexpr (ACROSS) {
+      const int64_t rows = left < kDepth ? left : kDepth;
+      const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p + r0 * o.pitch), 0,
+                                                         (uint32_t)((rows - 1) * o.pitch + (o.valid < R ? o.valid : R) * (int)sizeof(T)), 0x00027000);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)(lds + (i * W + wave) * 1024), 16, off[i], 0, 0, 0);
+    } else {
+      const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p), 0,
+                                                         (uint32_t)(((o.valid < R ? o.valid : R) - 1) * o.pitch + red * (int)sizeof(T)), 0x00027000);
+      const uint32_t base = (uint32_t)(r0 * sizeof(T));
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        uint32_t at = off[i];
+        if (left < kDepth) {                                              // (the row's end: the next row follows)
+          int row, chunk;
+          place(wave, lane, i, row, chunk);
+          if (chunk * kElem >= left) at = 0x80000000u;
+        }
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)(lds + (i * W + wave) * 1024), 16, at, base, 0, 0);
+      }
+    }
+  }
+  // Through registers: any alignment and any pitch.
+  __device__ __forceinline__ void fetch(const Operand& o, int64_t red, int64_t r0, word4 (&st)[kLoads], int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row, chunk;
+      place(wave, lane, i, row, chunk);
+      const int64_t r = ACROSS ? r0 + row : r0 + chunk * kElem;           // first summed index
+      const int q = ACROSS ? chunk * kElem : row;                         // row or column of the tile
+      const int64_t have = ACROSS ? (r < red ? o.valid - q : 0) : (q < o.valid ? red - r : 0);
+      const char* p = o.p + (ACROSS ? r : (int64_t)q) * o.pitch + (ACROSS ? (int64_t)q : r) * (int)sizeof(T);
+      word4 v = {0, 0, 0, 0};
+      if (have >= kElem) {
+        __builtin_memcpy(&v, p, 16);
+      } else if (have > 0) {
+        T e[kElem];
+#pragma unroll
+        for (int j = 0; j < kElem; ++j) e[j] = j < have ? reinterpret_cast<const T*>(p)[j] : (T)0.f;
+        __builtin_memcpy(&v, e, 16);
+      }
+      st[i] = v;
+    }
+  }
+  static __device__ __forceinline__ void put(const word4 (&st)[kLoads], char* lds, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<word4*>(lds + (i * W + wave) * 1024 + lane * 16) = st[i];
+  }
+  // Fragment of the 16 rows (columns) from `first` on, half `s` of the slab.
+  static __device__ __forceinline__ word4 fragment(const char* lds, int first, int s, int lane) {
+    const int l = lane & 15, q = lane >> 4;
+    if constexpr (!ACROSS) {
+      return *reinterpret_cast<const word4*>(lds + (first + l) * kSlab + (((s * 4 + q) ^ (l & 7)) * 16));
+    } else if constexpr (sizeof(T) == 2) {
+      word4 v;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int k = s * 32 + q * 8 + t * 4 + (l >> 2);
+        const char* p = lds + k * kRow + ((first * 2) ^ (turn(k) << 4)) + (l & 3) * 8;
+        const word2 d = __builtin_bit_cast(word2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p));
+        v[2 * t] = d[0];
+        v[2 * t + 1] = d[1];
+      }
+      return v;
+    } else {
+      word4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = s * 16 + q * 4 + j;
+        v[j] = *reinterpret_cast<const uint32_t*>(lds + k * kRow + (((first + l) * 4) ^ (turn(k) << 4)));
+      }
+      return v;
+    }
+  }
+};
+
+// Tile of BM x BN by WM x WN wavefronts.
+template <typename T, typename O, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
+struct Tile {
+  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+  static constexpr int MI = BM / WM / 16, NJ = BN / WN / 16;
+  using LA = Loader<T, AT, BM, kWaves>;
+  using LB = Loader<T, BT, BN, kWaves>;
+  static constexpr int kStage = LA::kBytes + LB::kBytes;
+  static constexpr int kLds = 2 * kStage;
+
+  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, int64_t ldc, char* lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int m0 = wave / WN * (MI * 16), n0 = wave % WN * (NJ * 16);
+    f32x4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto work = [&](const char* buf) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        word4 fa[MI], fb[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[j] = LB::fragment(buf + LA::kBytes, n0 + j * 16, s, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[i] = LA::fragment(buf, m0 + i * 16, s, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = multiply(T(), fb[j], fa[i], acc[i][j]);
+      }
+    };
+    const int64_t slabs = (red + LA::kDepth - 1) / LA::kDepth;
+    LA la;
+    LB lb;
+    if constexpr (DIRECT) {
+      la.init(a, wave, lane);
+      lb.init(b, wave, lane);
+      if (slabs > 0) {
+        la.direct(a, red, 0, lds, wave, lane);
+        lb.direct(b, red, 0, lds + LA::kBytes, wave, lane);
+      }
+      for (int64_t s = 0; s < slabs; ++s) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        char* next = lds + ((s + 1) & 1) * kStage;
+        if (s + 1 < slabs) {
+          la.direct(a, red, (s + 1) * LA::kDepth, next, wave, lane);
+          lb.direct(b, red, (s + 1) * LA::kDepth, next + LA::kBytes, wave, lane);
+        }
+        work(lds + (s & 1) * kStage);
+      }
+    } else {
+      word4 sa[LA::kLoads], sb[LB::kLoads];
+      if (slabs > 0) {
+        la.fetch(a, red, 0, sa, wave, lane);
+        lb.fetch(b, red, 0, sb, wave, lane);
+      }
+      for (int64_t s = 0; s < slabs; ++s) {
+        char* buf = lds + (s & 1) * kStage;
+        LA::put(sa, buf, wave, lane);
+        LB::put(sb, buf + LA::kBytes, wave, lane);
+        __syncthreads();
+        if (s + 1 < slabs) {
+          la.fetch(a, red, (s + 1) * LA::kDepth, sa, wave, lane);
+          lb.fetch(b, red, (s + 1) * LA::kDepth, sb, wave, lane);
+        }
+        work(buf);
+      }
+    }
+    // a lane holds four neighbouring columns of a row in each fragment
+    const int l = lane & 15, q = lane >> 4;
+    const bool wide = ((uintptr_t)c | (uintptr_t)(ldc * sizeof(O))) % (4 * sizeof(O)) == 0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int m = m0 + i * 16 + l;
+      if (m >= a.valid) continue;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int n = n0 + j * 16 + q * 4;
+        O* to = c + m * ldc + n;
+        if (wide && n + 4 <= b.valid) {
+          struct alignas(4 * sizeof(O)) Four { O e[4]; } v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v.e[r] = from_float<O>(acc[i][j][r]);
+          *reinterpret_cast<Four*>(to) = v;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < b.valid) to[r] = from_float<O>(acc[i][j][r]);
+        }
+      }
+    }
+  }
+};
+
+// Blocks go to the eight dies in turn: each die gets neighbouring tiles, whose operands its cache then holds.  Tiles are taken
+// down bands of four slices of rows, so that those of one band share their columns' operand while it is there.
+__device__ __forceinline__ bool tile_of(int64_t block, int64_t down, int64_t across, int64_t& i, int64_t& j) {
+  const int64_t total = down * across, per = (total + 7) / 8;
+  const int64_t t = block % 8 * per + block / 8;
+  if (t >= total) return false;
+  const int64_t band = t / (4 * across), rest = t - band * 4 * across;
+  const int64_t height = down - band * 4 < 4 ? down - band * 4 : 4;
+  i = band * 4 + rest % height;
+  j = rest / height;
+  return true;
+}
+inline int64_t tile_blocks(int64_t tiles) { return (tiles + 7) / 8 * 8; }
+
+template <typename T, typename O, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN) k_rows_product(ProductArgs p) {
+  using K = Tile<T, O, false, BT, BM, BN, WM, WN, DIRECT>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int cols = BT ? p.k : p.n, red = BT ? p.n : p.k;
+  int64_t number, j;
+  if (!tile_of(blockIdx.x, p.slices, (cols + BN - 1) / BN, number, j)) return;
+  const Slice s = find_slice(p.offsets, p.groups, p.rows, p.each, p.shift, number);
   if (s.group < 0 || s.end <= s.begin) return;
-  const int cols = TRANSPOSED ? p.k : p.n, red = TRANSPOSED ? p.n : p.k;
-  const int c0 = blockIdx.x * 64;
-  const T* b = (const T*)p.b + s.group * p.gsb;
-  tile_product<T, O>((const T*)p.a + s.begin * p.lda, p.lda, 1, (int)(s.end - s.begin), TRANSPOSED ? b + c0 : b + c0 * p.ldb,
-                     TRANSPOSED ? 1 : p.ldb, TRANSPOSED ? p.ldb : 1, cols - c0, red, (O*)p.c + s.begin * p.ldc + c0, p.ldc);
+  const int64_t c0 = j * BN;
+  const Operand a{(const char*)p.a + s.begin * p.lda * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(s.end - s.begin)};
+  const Operand b{(const char*)p.b + (s.group * p.gsb + (BT ? c0 : c0 * p.ldb)) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(cols - c0)};
+  K::run(a, b, red, (O*)p.c + s.begin * p.ldc + c0, p.ldc, lds);
 }
 
-template <typename T, typename O>
-__global__ void __launch_bounds__(256) k_group_product(ProductArgs p) {
-  const int64_t g = blockIdx.z;
+template <typename T, typename O, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN) k_group_product(ProductArgs p) {
+  using K = Tile<T, O, true, true, BM, BN, WM, WN, DIRECT>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int64_t tn = (p.n + BM - 1) / BM, tk = (p.k + BN - 1) / BN;
+  int64_t i, j;
+  if (!tile_of(blockIdx.x, p.groups * tn, tk, i, j)) return;
+  const int64_t g = i / tn, n0 = (i - g * tn) * BM, k0 = j * BN;
   const int64_t first = offset_at(p.offsets, g, p.rows);
   int64_t last = offset_at(p.offsets, g + 1, p.rows);
   if (last < first) last = first;
-  const int n0 = blockIdx.y * 64, k0 = blockIdx.x * 64;
-  tile_product<T, O>((const T*)p.a + first * p.lda + n0, 1, p.lda, p.n - n0, (const T*)p.b + first * p.ldb + k0, 1, p.ldb, p.k - k0,
-                     last - first, (O*)p.c + g * p.gsc + n0 * p.ldc + k0, p.ldc);
+  const Operand a{(const char*)p.a + (first * p.lda + n0) * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(p.n - n0)};
+  const Operand b{(const char*)p.b + (first * p.ldb + k0) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(p.k - k0)};
+  K::run(a, b, last - first, (O*)p.c + g * p.gsc + n0 * p.ldc + k0, p.ldc, lds);
 }
 
 int check_sizes(int32_t product, int64_t rows, int64_t groups, int64_t n, int64_t k) {
@@ -72,16 +320,37 @@ int check_sizes(int32_t product, int64_t rows, int64_t groups, int64_t n, int64_
   return ADACGD_OK;
 }
 
-template <typename T, typename O>
-int launch(int32_t product, const ProductArgs& p, hipStream_t stream) {
-  if (product == ADACGD_DW) {
-    k_group_product<T, O><<<dim3((p.k + 63) / 64, (p.n + 63) / 64, p.groups), 256, 0, stream>>>(p);
-  } else {
-    const int64_t slices = slice_numbers(p.rows, p.groups, kTileShift);
-    if (product == ADACGD_FORWARD) k_rows_product<T, O, false><<<dim3((p.n + 63) / 64, slices), 256, 0, stream>>>(p);
-    else k_rows_product<T, O, true><<<dim3((p.k + 63) / 64, slices), 256, 0, stream>>>(p);
+template <typename K>
+int enqueue(K kernel, int64_t blocks, int threads, int lds, hipStream_t stream, const ProductArgs& p) {
+  if (blocks > kMaxCount / 512) return fail(ADACGD_ERR_ARG, "more tiles than one launch takes");
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return fail(ADACGD_ERR_DEVICE, "adacgd_group_matmul: %s", hipGetErrorString(e));
   }
+  kernel<<<blocks, threads, lds, stream>>>(p);
   return launched("adacgd_group_matmul");
+}
+
+template <typename T, typename O, int BM, int BN, int WM, int WN, bool DIRECT>
+int launch(int32_t product, ProductArgs p, hipStream_t stream) {
+  if (product == ADACGD_DW) {
+    using K = Tile<T, O, true, true, BM, BN, WM, WN, DIRECT>;
+    const int64_t tiles = p.groups * ((p.n + BM - 1) / BM) * ((p.k + BN - 1) / BN);
+    return enqueue(k_group_product<T, O, BM, BN, WM, WN, DIRECT>, tile_blocks(tiles), K::kThreads, K::kLds, stream, p);
+  }
+  p.shift = __builtin_ctz(BM);
+  p.slices = slice_numbers(p.rows, p.groups, p.shift);
+  using K = Tile<T, O, false, true, BM, BN, WM, WN, DIRECT>;
+  const int64_t blocks = tile_blocks(p.slices * (((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN));
+  if (product == ADACGD_FORWARD) return enqueue(k_rows_product<T, O, false, BM, BN, WM, WN, DIRECT>, blocks, K::kThreads, K::kLds, stream, p);
+  return enqueue(k_rows_product<T, O, true, BM, BN, WM, WN, DIRECT>, blocks, K::kThreads, K::kLds, stream, p);
+}
+
+// Rows begin on 16 bytes and are whole 16 bytes, and a tile's rows are less than 2^31 bytes apart.
+bool straight(const adacgd_tensor* t, int64_t rows, int64_t columns, bool grouped) {
+  const int64_t e = dtype_size(t->dtype);
+  return (uintptr_t)t->data % 16 == 0 && columns * e % 16 == 0 && (rows <= 1 || (t->stride * e % 16 == 0 && t->stride * e <= (int64_t(1) << 22))) &&
+         (!grouped || t->group_stride * e % 16 == 0);
 }
 
 }  // namespace
@@ -114,12 +383,22 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
   ADACGD_TRY(adacgd_group_matmul_workspace_bytes(product, a->dtype, rows, groups, n, k, &need));
   ADACGD_TRY(check_workspace(workspace, workspace_bytes, need));
   if (rows == 0 && !dw) return ADACGD_OK;
-  ProductArgs p{a->data, b->data, c->data, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, (int)n, (int)k};
+  ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, 0, (int)n, (int)k, 0};
   if (!dw && b->group_stride == 0) { p.each = groups; p.groups = 1; }      // one matrix for all: one group
+  const bool direct = straight(a, rows, product == ADACGD_FORWARD ? k : n, false) && straight(b, dw ? rows : n, k, !dw);
+  const bool large = direct && rows / p.groups >= 256 && n >= 256 && k >= 256;
   return by_dtype(a->dtype, [&](auto t) {
     using T = decltype(t);
-    if (c->dtype == ADACGD_FP32) return launch<T, float>(product, p, (hipStream_t)stream);
-    return launch<T, T>(product, p, (hipStream_t)stream);
+    const auto go = [&](auto o) {
+      using O = decltype(o);
+      if constexpr (sizeof(T) == 2) {
+        if (large) return launch<T, O, 256, 256, 2, 4, true>(product, p, (hipStream_t)stream);
+      }
+      if (direct) return launch<T, O, 128, 128, 2, 2, true>(product, p, (hipStream_t)stream);
+      return launch<T, O, 128, 128, 2, 2, false>(product, p, (hipStream_t)stream);
+    };
+    if (c->dtype == ADACGD_FP32) return go(float());
+    return go(T());
   });
 }
 
