@@ -27,6 +27,34 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSlab = 128;      // bytes of the summed index
 
+// Blocks go to the eight dies in turn.  Tiles are dealt to the dies in patches of 32, one for each compute unit of a die, so that
+// those at work on a die at one time share rows and columns in its cache; patches, not long runs of tiles, so that each die
+// gets its share of the numbers that no slice has and of long groups.  A patch is 1 << lw tiles wide: 4 x 8, or as the
+// matrix allows.
+struct Patches {
+  int64_t down, across;
+  int lw;
+};
+inline Patches patches_of(int64_t down, int64_t across) {
+  int lw = 3;
+  while (lw > 0 && int64_t(1) << (lw - 1) >= across) --lw;
+  while (lw < 5 && int64_t(1) << (5 - lw - 1) >= down) ++lw;
+  return Patches{down, across, lw};
+}
+__host__ __device__ inline int64_t patch_columns(const Patches& p) { return (p.across + (1 << p.lw) - 1) >> p.lw; }
+inline int64_t patch_blocks(const Patches& p) {
+  const int64_t rows = (p.down + (32 >> p.lw) - 1) / (32 >> p.lw);
+  return (rows * patch_columns(p) + 7) / 8 * 8 * 32;
+}
+__device__ __forceinline__ bool tile_of(uint32_t block, const Patches& p, int64_t& i, int64_t& j) {
+  const uint32_t columns = (uint32_t)patch_columns(p);
+  const uint32_t patch = (block >> 8) * 8 + (block & 7), in = block >> 3 & 31;
+  const uint32_t row = patch / columns;
+  i = (int64_t)row * (32 >> p.lw) + (in >> p.lw);
+  j = ((int64_t)(patch - row * columns) << p.lw) + (in & ((1u << p.lw) - 1));
+  return i < p.down && j < p.across;
+}
+
 struct ProductArgs {
   const void* a;
   const void* b;
@@ -35,7 +63,7 @@ struct ProductArgs {
   const int64_t* offsets;
   int64_t rows, groups, each;           // `each` entries of offsets to a group
   int64_t lda, ldb, ldc, gsb, gsc;
-  int64_t slices;                       // numbers of slices
+  Patches patches;
   int n, k, shift;
 };
 
@@ -70,7 +98,7 @@ struct Loader {
 
   // where pieces of row `k` are put, in chunks
   static __device__ __forceinline__ int turn(int k) {
-    if (!ACROSS) return k & 7;
+    if (!ACROSS) return (k >> 1 & 1) * 2 + (k >> 3 & 1) * 4;
     return sizeof(T) == 2 ? ((k & 3) + ((k >> 3 & 1) << 2)) << 1 : (k >> 2 & 3) << 2;
   }
   // row in LDS and chunk of that row's memory that the lane's i-th 16 bytes hold
@@ -103,15 +131,18 @@ struct Loader {
       const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p), 0,
                                                          (uint32_t)(((o.valid < R ? o.valid : R) - 1) * o.pitch + red * (int)sizeof(T)), 0x00027000);
       const uint32_t base = (uint32_t)(r0 * sizeof(T));
+      if (left >= kDepth) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        uint32_t at = off[i];
-        if (left < kDepth) {                                              // (the row's end: the next row follows)
+        for (int i = 0; i < kLoads; ++i)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)(lds + (i * W + wave) * 1024), 16, off[i], base, 0, 0);
+      } else {                                                            // (the rows' ends: the next rows follow)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
           int row, chunk;
           place(wave, lane, i, row, chunk);
-          if (chunk * kElem >= left) at = 0x80000000u;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)(lds + (i * W + wave) * 1024), 16,
+                                                   chunk * kElem < (int)left ? off[i] : 0x80000000u, base, 0, 0);
         }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)(lds + (i * W + wave) * 1024), 16, at, base, 0, 0);
       }
     }
   }
@@ -145,7 +176,7 @@ struct Loader {
   static __device__ __forceinline__ word4 fragment(const char* lds, int first, int s, int lane) {
     const int l = lane & 15, q = lane >> 4;
     if constexpr (!ACROSS) {
-      return *reinterpret_cast<const word4*>(lds + (first + l) * kSlab + (((s * 4 + q) ^ (l & 7)) * 16));
+      return *reinterpret_cast<const word4*>(lds + (first + l) * kSlab + (((s * 4 + q) ^ turn(l)) * 16));
     } else if constexpr (sizeof(T) == 2) {
       word4 v;
 #pragma unroll
@@ -169,15 +200,49 @@ struct Loader {
   }
 };
 
+// Writes 64 x 64 of C, whose first `rows` and `columns` exist, from a wavefront's fragments: a lane holds four neighbouring
+// columns of a row in each, pieces of 32 bytes of 16 rows an instruction.  They go through LDS (64 rows of 64 elements, the
+// wavefront's own), so that whole lines are written: straight from the fragments a tile of 256 x 256 took 28 us to write.
+constexpr int kStoreBytes = 64 * 64;      // ... times the size of an element
+template <typename O>
+__device__ __forceinline__ void store(const f32x4 (&acc)[4][4], O* c, int64_t ldc, int rows, int columns, char* lds, int lane) {
+  constexpr int pitch = 64 * (int)sizeof(O), chunks = pitch / 16, elems = 16 / (int)sizeof(O);
+  const int l = lane & 15, q = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      struct alignas(4 * sizeof(O)) Four { O e[4]; } v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v.e[r] = from_float<O>(acc[i][j][r]);
+      const int byte = (j * 16 + q * 4) * (int)sizeof(O);
+      *reinterpret_cast<Four*>(lds + (i * 16 + l) * pitch + ((byte / 16 ^ (l & 7)) * 16) + byte % 16) = v;
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (((uintptr_t)c | (uintptr_t)(ldc * sizeof(O)) | (uintptr_t)(columns < 64 ? columns * sizeof(O) : 0)) % 16 == 0) {
+#pragma unroll
+    for (int t = 0; t < chunks; ++t) {
+      const int row = t * (64 / chunks) + lane / chunks, chunk = lane % chunks;
+      const word4 v = *reinterpret_cast<const word4*>(lds + row * pitch + ((chunk ^ (row & 7)) * 16));
+      if (row < rows && chunk * elems < columns) *reinterpret_cast<word4*>(c + row * ldc + chunk * elems) = v;
+    }
+  } else {
+    const int byte = lane * (int)sizeof(O);
+    for (int row = 0; row < (rows < 64 ? rows : 64); ++row)
+      if (lane < columns) c[row * ldc + lane] = *reinterpret_cast<const O*>(lds + row * pitch + ((byte / 16 ^ (row & 7)) * 16) + byte % 16);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // Tile of BM x BN by WM x WN wavefronts.
 template <typename T, typename O, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
 struct Tile {
-  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, kRows = BM, kColumns = BN;
   static constexpr int MI = BM / WM / 16, NJ = BN / WN / 16;
   using LA = Loader<T, AT, BM, kWaves>;
   using LB = Loader<T, BT, BN, kWaves>;
   static constexpr int kStage = LA::kBytes + LB::kBytes;
-  static constexpr int kLds = 2 * kStage;
+  static constexpr int kLds = 2 * kStage > kWaves * kStoreBytes * (int)sizeof(O) ? 2 * kStage : kWaves * kStoreBytes * (int)sizeof(O);
 
   static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, int64_t ldc, char* lds) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
@@ -240,53 +305,109 @@ struct Tile {
         work(buf);
       }
     }
-    // a lane holds four neighbouring columns of a row in each fragment
-    const int l = lane & 15, q = lane >> 4;
-    const bool wide = ((uintptr_t)c | (uintptr_t)(ldc * sizeof(O))) % (4 * sizeof(O)) == 0;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int m = m0 + i * 16 + l;
-      if (m >= a.valid) continue;
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int n = n0 + j * 16 + q * 4;
-        O* to = c + m * ldc + n;
-        if (wide && n + 4 <= b.valid) {
-          struct alignas(4 * sizeof(O)) Four { O e[4]; } v;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v.e[r] = from_float<O>(acc[i][j][r]);
-          *reinterpret_cast<Four*>(to) = v;
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (n + r < b.valid) to[r] = from_float<O>(acc[i][j][r]);
-        }
-      }
-    }
+    static_assert(MI == 4 && NJ == 4, "");
+    __syncthreads();                                                   // (the slabs have been read)
+    store<O>(acc, c + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
   }
 };
 
-// Blocks go to the eight dies in turn: each die gets neighbouring tiles, whose operands its cache then holds.  Tiles are taken
-// down bands of four slices of rows, so that those of one band share their columns' operand while it is there.
-__device__ __forceinline__ bool tile_of(int64_t block, int64_t down, int64_t across, int64_t& i, int64_t& j) {
-  const int64_t total = down * across, per = (total + 7) / 8;
-  const int64_t t = block % 8 * per + block / 8;
-  if (t >= total) return false;
-  const int64_t band = t / (4 * across), rest = t - band * 4 * across;
-  const int64_t height = down - band * 4 < 4 ? down - band * 4 : 4;
-  i = band * 4 + rest % height;
-  j = rest / height;
-  return true;
-}
-inline int64_t tile_blocks(int64_t tiles) { return (tiles + 7) / 8 * 8; }
+// Tile of 256 x 256 for 16-bit types by eight wavefronts, two on each SIMD: while one of them multiplies, the other reads its
+// next fragments.  A wavefront does its 128 x 64 in two halves of a slab; each half is a phase that reads fragments and has
+// loads begin, a barrier, a phase of 32 matrix instructions, a barrier.  The wavefronts of the lower half of the tile go one
+// barrier behind the others.
+//   LDS holds five operands' slabs (160 KB), in the order A0 B0 A1 B1 ...: those of the slab multiplied and the three that come
+//   next.  In slab s, when the slots of slab s - 1 are free, the loads of B of s + 1 and A of s + 2 begin.  All wavefronts have
+//   read their last fragments of s - 1 then: they wait for these before a barrier, the later ones one phase before the others
+//   begin slab s.  A slab's loads are waited for in the last reading phase before it, whose end every wavefront reaches before
+//   the first of them reads the slab.
+// Slabs are whole lines of 128 bytes: with 64 bytes a load of rows made twice the requests, and it is requests (some 110 of
+// them on their way from a compute unit) that bound the loads: 8192^3 took 820 us for its loads alone, 600 where rows of
+// 512 bytes are read.
+template <typename T, typename O, bool AT, bool BT>
+struct Wide {
+  static constexpr int kThreads = 512, kRows = 256, kColumns = 256;
+  using LA = Loader<T, AT, 256, 8>;
+  using LB = Loader<T, BT, 256, 8>;
+  static constexpr int kSlot = LA::kBytes, kSlots = 5, kLds = kSlots * kSlot;
 
-template <typename T, typename O, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN) k_rows_product(ProductArgs p) {
-  using K = Tile<T, O, false, BT, BM, BN, WM, WN, DIRECT>;
+  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, int64_t ldc, char* lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int m0 = wave / 4 * 128, n0 = wave % 4 * 64;
+    f32x4 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int slabs = (int)((red + LA::kDepth - 1) / LA::kDepth);
+    LA la;
+    LB lb;
+    la.init(a, wave, lane);
+    lb.init(b, wave, lane);
+    const auto load_a = [&](int s, int slot) { la.direct(a, red, (int64_t)s * LA::kDepth, lds + slot * kSlot, wave, lane); };
+    const auto load_b = [&](int s, int slot) { lb.direct(b, red, (int64_t)s * LB::kDepth, lds + slot * kSlot, wave, lane); };
+    const auto barrier = [&] {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+    };
+    const auto wait_loads = [&](bool more) {                           // for all but those of one operand's slab
+      if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::kLoads) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    if (slabs > 0) {
+      load_a(0, 0);
+      load_b(0, 1);
+      if (slabs > 1) load_a(1, 2);
+    }
+    wait_loads(slabs > 1);
+    barrier();
+    if (wave >= 4) barrier();
+    int at = 0;                                                        // slot of A
+    const auto slot = [&](int k) { return at + k < kSlots ? at + k : at + k - kSlots; };
+    for (int s = 0; s < slabs; ++s) {
+      const char* as = lds + at * kSlot;
+      const char* bs = lds + slot(1) * kSlot;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        word4 fa[8], fb[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fb[j] = LB::fragment(bs, n0 + j * 16, h, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fa[i] = LA::fragment(as, m0 + i * 16, h, lane);
+        if (h == 0) {
+          if (s + 1 < slabs) load_b(s + 1, slot(3));
+        } else {
+          if (s + 2 < slabs) load_a(s + 2, slot(4));
+          wait_loads(s + 2 < slabs);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] = multiply(T(), fb[j], fa[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+        barrier();
+      }
+      at = slot(2);
+    }
+    if (wave < 4) barrier();                                           // (and the slabs have been read)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      store<O>(reinterpret_cast<const f32x4(&)[4][4]>(acc[h * 4]), c + (m0 + h * 64) * ldc + n0, ldc, a.valid - m0 - h * 64, b.valid - n0,
+               lds + wave * kStoreBytes * sizeof(O), lane);
+  }
+};
+
+template <typename T, typename O, bool BT, typename K>
+__global__ void __launch_bounds__(K::kThreads) k_rows_product(ProductArgs p) {
+  constexpr int BN = K::kColumns;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int cols = BT ? p.k : p.n, red = BT ? p.n : p.k;
   int64_t number, j;
-  if (!tile_of(blockIdx.x, p.slices, (cols + BN - 1) / BN, number, j)) return;
+  if (!tile_of(blockIdx.x, p.patches, number, j)) return;
   const Slice s = find_slice(p.offsets, p.groups, p.rows, p.each, p.shift, number);
   if (s.group < 0 || s.end <= s.begin) return;
   const int64_t c0 = j * BN;
@@ -295,13 +416,13 @@ __global__ void __launch_bounds__(64 * WM * WN) k_rows_product(ProductArgs p) {
   K::run(a, b, red, (O*)p.c + s.begin * p.ldc + c0, p.ldc, lds);
 }
 
-template <typename T, typename O, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN) k_group_product(ProductArgs p) {
-  using K = Tile<T, O, true, true, BM, BN, WM, WN, DIRECT>;
+template <typename T, typename O, typename K>
+__global__ void __launch_bounds__(K::kThreads) k_group_product(ProductArgs p) {
+  constexpr int BM = K::kRows, BN = K::kColumns;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int64_t tn = (p.n + BM - 1) / BM, tk = (p.k + BN - 1) / BN;
+  const int64_t tn = (p.n + BM - 1) / BM;
   int64_t i, j;
-  if (!tile_of(blockIdx.x, p.groups * tn, tk, i, j)) return;
+  if (!tile_of(blockIdx.x, p.patches, i, j)) return;
   const int64_t g = i / tn, n0 = (i - g * tn) * BM, k0 = j * BN;
   const int64_t first = offset_at(p.offsets, g, p.rows);
   int64_t last = offset_at(p.offsets, g + 1, p.rows);
@@ -331,20 +452,26 @@ int enqueue(K kernel, int64_t blocks, int threads, int lds, hipStream_t stream, 
   return launched("adacgd_group_matmul");
 }
 
-template <typename T, typename O, int BM, int BN, int WM, int WN, bool DIRECT>
+// K<AT, BT>: the tile with each operand along or across.
+template <typename T, typename O, template <bool, bool> class K>
 int launch(int32_t product, ProductArgs p, hipStream_t stream) {
+  constexpr int BM = K<true, true>::kRows, BN = K<true, true>::kColumns, threads = K<true, true>::kThreads, lds = K<true, true>::kLds;
   if (product == ADACGD_DW) {
-    using K = Tile<T, O, true, true, BM, BN, WM, WN, DIRECT>;
-    const int64_t tiles = p.groups * ((p.n + BM - 1) / BM) * ((p.k + BN - 1) / BN);
-    return enqueue(k_group_product<T, O, BM, BN, WM, WN, DIRECT>, tile_blocks(tiles), K::kThreads, K::kLds, stream, p);
+    p.patches = patches_of(p.groups * ((p.n + BM - 1) / BM), (p.k + BN - 1) / BN);
+    return enqueue(k_group_product<T, O, K<true, true>>, patch_blocks(p.patches), threads, lds, stream, p);
   }
   p.shift = __builtin_ctz(BM);
-  p.slices = slice_numbers(p.rows, p.groups, p.shift);
-  using K = Tile<T, O, false, true, BM, BN, WM, WN, DIRECT>;
-  const int64_t blocks = tile_blocks(p.slices * (((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN));
-  if (product == ADACGD_FORWARD) return enqueue(k_rows_product<T, O, false, BM, BN, WM, WN, DIRECT>, blocks, K::kThreads, K::kLds, stream, p);
-  return enqueue(k_rows_product<T, O, true, BM, BN, WM, WN, DIRECT>, blocks, K::kThreads, K::kLds, stream, p);
+  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), ((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN);
+  const int64_t blocks = patch_blocks(p.patches);
+  if (product == ADACGD_FORWARD) return enqueue(k_rows_product<T, O, false, K<false, false>>, blocks, threads, lds, stream, p);
+  return enqueue(k_rows_product<T, O, true, K<false, true>>, blocks, threads, lds, stream, p);
 }
+template <typename T, typename O>
+struct Tiles {
+  template <bool AT, bool BT> using Large = Wide<T, O, AT, BT>;
+  template <bool AT, bool BT> using Direct = Tile<T, O, AT, BT, 128, 128, 2, 2, true>;
+  template <bool AT, bool BT> using Staged = Tile<T, O, AT, BT, 128, 128, 2, 2, false>;
+};
 
 // Rows begin on 16 bytes and are whole 16 bytes, and a tile's rows are less than 2^31 bytes apart.
 bool straight(const adacgd_tensor* t, int64_t rows, int64_t columns, bool grouped) {
@@ -383,7 +510,7 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
   ADACGD_TRY(adacgd_group_matmul_workspace_bytes(product, a->dtype, rows, groups, n, k, &need));
   ADACGD_TRY(check_workspace(workspace, workspace_bytes, need));
   if (rows == 0 && !dw) return ADACGD_OK;
-  ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, 0, (int)n, (int)k, 0};
+  ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, {}, (int)n, (int)k, 0};
   if (!dw && b->group_stride == 0) { p.each = groups; p.groups = 1; }      // one matrix for all: one group
   const bool direct = straight(a, rows, product == ADACGD_FORWARD ? k : n, false) && straight(b, dw ? rows : n, k, !dw);
   const bool large = direct && rows / p.groups >= 256 && n >= 256 && k >= 256;
@@ -392,10 +519,10 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
     const auto go = [&](auto o) {
       using O = decltype(o);
       if constexpr (sizeof(T) == 2) {
-        if (large) return launch<T, O, 256, 256, 2, 4, true>(product, p, (hipStream_t)stream);
+        if (large) return launch<T, O, Tiles<T, O>::template Large>(product, p, (hipStream_t)stream);
       }
-      if (direct) return launch<T, O, 128, 128, 2, 2, true>(product, p, (hipStream_t)stream);
-      return launch<T, O, 128, 128, 2, 2, false>(product, p, (hipStream_t)stream);
+      if (direct) return launch<T, O, Tiles<T, O>::template Direct>(product, p, (hipStream_t)stream);
+      return launch<T, O, Tiles<T, O>::template Staged>(product, p, (hipStream_t)stream);
     };
     if (c->dtype == ADACGD_FP32) return go(float());
     return go(T());
