@@ -393,7 +393,7 @@ int adacgd_layer_norm(int64_t rows, int64_t d, const adacgd_tensor* x, const flo
                       const adacgd_tensor* y, float* mean, float* rstd, void* stream);
 
 /* Its gradients: dx for the rows of all groups, and for every group the gradients of weight and bias from its own rows,
- * dweight, dbias: fp32 [groups x d] (an empty group's are zero), each may be NULL.  dy and dx have the type of x. */
+ * dweight, dbias: fp32 [groups x d] (an empty group's are zero), each may be NULL.  dy and dx have the type of x; offsets may be NULL with one group, which then is all rows. */
 int adacgd_layer_norm_backward_workspace_bytes(int64_t rows, int64_t groups, int64_t d, int64_t* bytes);
 int adacgd_layer_norm_backward(int64_t rows, int64_t groups, int64_t d, const int64_t* offsets, const adacgd_tensor* dy,
                                const adacgd_tensor* x, const float* weight, const float* mean, const float* rstd,

@@ -70,6 +70,14 @@ __device__ __forceinline__ int64_t offset_at(const int64_t* offsets, int64_t i, 
 // offsets make one group.
 __device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t groups, int64_t rows, int64_t each, int shift, int64_t number) {
   Slice s{-1, 0, 0, 0, 0};
+  if (!offsets) {                                         // one group of all rows
+    s.last = rows;
+    s.begin = number << shift;
+    if (s.begin >= rows && number > 0) return s;
+    s.group = 0;
+    s.end = s.begin + (int64_t(1) << shift) < rows ? s.begin + (int64_t(1) << shift) : rows;
+    return s;
+  }
   int64_t low = 0, count = groups;
   const int lane = (int)lane_id();
   for (;;) {
@@ -93,6 +101,46 @@ __device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t grou
   s.end = s.begin + (int64_t(1) << shift) < s.last ? s.begin + (int64_t(1) << shift) : s.last;
   return s;
 }
+
+// First number of a group's slices.
+__device__ __forceinline__ int64_t first_number(int64_t first_row, int64_t group, int shift) { return (first_row >> shift) + group; }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or0f(float v) { return __uint_as_float(dpp_or0<CTRL, ROWS>(__float_as_uint(v))); }
+// Sum over the wavefront, in every lane.
+__device__ __forceinline__ float wave_sumf(float v) {
+  v += dpp_or0f<kDppShr + 1, 0xf>(v);
+  v += dpp_or0f<kDppShr + 2, 0xf>(v);
+  v += dpp_or0f<kDppShr + 4, 0xf>(v);
+  v += dpp_or0f<kDppShr + 8, 0xf>(v);
+  v += dpp_or0f<kDppBcast15, 0xa>(v);
+  v += dpp_or0f<kDppBcast31, 0xc>(v);
+  return __uint_as_float(lane_value(__float_as_uint(v), 63));
+}
+
+// 16 bytes of a row at any alignment; a vector that passes the row's end is taken element by element (zero behind it).
+template <typename T>
+struct Vec {
+  static constexpr int kElems = 16 / sizeof(T);
+  T e[kElems];
+  __device__ __forceinline__ void load(const T* p, int64_t have) {
+    if (have >= kElems) {
+      __builtin_memcpy(e, p, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kElems; ++j) e[j] = j < have ? p[j] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int64_t have) const {
+    if (have >= kElems) {
+      __builtin_memcpy(p, e, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kElems; ++j)
+        if (j < have) p[j] = e[j];
+    }
+  }
+};
 
 // Element types: what is stored, and its value as a float.
 template <typename T>

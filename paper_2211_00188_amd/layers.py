@@ -185,9 +185,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, offsets=None, dx=None, dweigh
     import torch
     _gpu("x", x, 2)
     rows, d = x.shape
-    if offsets is None:
-        offsets = torch.arange(2, device=x.device) * rows
-    off, groups = _offsets(offsets, x), offsets.numel() - 1
+    off, groups = (None, 1) if offsets is None else (_offsets(offsets, x), offsets.numel() - 1)
     tx, tdy = _matrix("x", x, rows, d), _matrix("dy", dy, rows, d, x)
     w = None if weight is None else _vector("weight", weight, d, torch.float32, x)
     m, r = _vector("mean", mean, rows, torch.float32, x), _vector("rstd", rstd, rows, torch.float32, x)
