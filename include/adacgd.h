@@ -358,7 +358,7 @@ const char* adacgd_last_error(const adacgd_ctx* ctx);
  *    keeps anything.  All of them may be captured into a graph.  A workspace is needed until the enqueued work has
  *    completed and must not be shared by calls that may run at the same time; it need not be cleared.
  *  - Outputs must not overlap inputs or each other, except where stated.
- *  - Limits: rows below 2^31, at most 65535 groups, rows of at most 2^24 elements, strides below 2^31. */
+ *  - Limits: rows below 2^31, at most 65535 groups or 2^22 pairs, rows of at most 2^24 elements, strides below 2^31. */
 enum adacgd_dtype { ADACGD_FP32 = 0, ADACGD_BF16 = 1, ADACGD_FP16 = 2 };
 
 typedef struct {

@@ -107,6 +107,14 @@ __device__ __forceinline__ int64_t first_number(int64_t first_row, int64_t group
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_or0f(float v) { return __uint_as_float(dpp_or0<CTRL, ROWS>(__float_as_uint(v))); }
+// Sum over 16 neighbouring lanes, in all of them (by rotations of such a row).
+__device__ __forceinline__ float row16_sumf(float v) {
+  v += dpp_or0f<0x128, 0xf>(v);
+  v += dpp_or0f<0x124, 0xf>(v);
+  v += dpp_or0f<0x122, 0xf>(v);
+  v += dpp_or0f<0x121, 0xf>(v);
+  return v;
+}
 // Sum over the wavefront, in every lane.
 __device__ __forceinline__ float wave_sumf(float v) {
   v += dpp_or0f<kDppShr + 1, 0xf>(v);
@@ -118,35 +126,66 @@ __device__ __forceinline__ float wave_sumf(float v) {
   return __uint_as_float(lane_value(__float_as_uint(v), 63));
 }
 
-// 16 bytes of a row at any alignment; a vector that passes the row's end is taken element by element (zero behind it).
-template <typename T>
-struct Vec {
-  static constexpr int kElems = 16 / sizeof(T);
-  T e[kElems];
-  __device__ __forceinline__ void load(const T* p, int64_t have) {
-    if (have >= kElems) {
-      __builtin_memcpy(e, p, 16);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kElems; ++j) e[j] = j < have ? p[j] : (T)0.f;
-    }
-  }
-  __device__ __forceinline__ void store(T* p, int64_t have) const {
-    if (have >= kElems) {
-      __builtin_memcpy(p, e, 16);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kElems; ++j)
-        if (j < have) p[j] = e[j];
-    }
-  }
-};
-
 // Element types: what is stored, and its value as a float.
 template <typename T>
 __device__ __forceinline__ float to_float(T v) { return (float)v; }
 template <typename T>
 __device__ __forceinline__ T from_float(float v) { return (T)v; }      // (to nearest, ties to even)
+
+// 16 bytes of a row at any alignment; a vector that passes the row's end is taken element by element (`missing` behind it).  Kept as
+// words: where elements of the two ways to load it met, the compiler would wait for the load at once to take them apart.
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+template <typename T>
+struct Vec {
+  static constexpr int kElems = 16 / sizeof(T);
+  word4 w;
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    else if constexpr (__is_same(T, __bf16)) return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+    else return to_float(__builtin_bit_cast(T, (uint16_t)(j & 1 ? w[j / 2] >> 16 : w[j / 2])));
+  }
+  __device__ __forceinline__ void put(const float (&f)[kElems]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(f[j]);
+    } else {
+      typedef T pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = __builtin_bit_cast(uint32_t, pair{from_float<T>(f[2 * j]), from_float<T>(f[2 * j + 1])});
+    }
+  }
+  static __device__ __forceinline__ uint32_t bits(T v) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(uint32_t, v);
+    else return __builtin_bit_cast(uint16_t, v);
+  }
+  __device__ __forceinline__ void load(const T* p, int64_t have, float missing = 0.f) {
+    if (have >= kElems) {
+      __builtin_memcpy(&w, p, 16);
+      return;
+    }
+    w = word4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < kElems; ++j) {
+      const uint32_t u = bits(j < have ? p[j] : from_float<T>(missing));
+      if constexpr (sizeof(T) == 4) w[j] = u;
+      else w[j / 2] |= u << (16 * (j & 1));
+    }
+  }
+  // What was computed from the elements is computed again after this, not kept in registers of twice their size.
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(w)); }
+  __device__ __forceinline__ void store(T* p, int64_t have) const {
+    if (have >= kElems) {
+      __builtin_memcpy(p, &w, 16);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < kElems; ++j) {
+      if (j >= have) break;
+      if constexpr (sizeof(T) == 4) p[j] = __uint_as_float(w[j]);
+      else p[j] = __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j & 1))));
+    }
+  }
+};
 
 // f(type tag) for the C type of a dtype.
 template <typename F>

@@ -14,6 +14,7 @@ namespace {
 // x and one over y, or over dy, x and dx.
 template <int TPR, int BLOCK>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
+  if constexpr (TPR == 16) return row16_sumf(v);
   v = wave_sumf(v);
   if constexpr (TPR == 64) return v;
   __syncthreads();
@@ -27,6 +28,11 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
 // Two sums at once.
 template <int TPR, int BLOCK>
 __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {
+  if constexpr (TPR == 16) {
+    a = row16_sumf(a);
+    b = row16_sumf(b);
+    return;
+  }
   a = wave_sumf(a);
   b = wave_sumf(b);
   if constexpr (TPR == 64) return;
@@ -58,30 +64,41 @@ __global__ void __launch_bounds__(BLOCK) k_norm(const T* x, int64_t ldx, const f
   float w[NV][E], b[NV][E];
   load_columns<NV, E, TPR>(weight, 1.f, t, d, w);
   load_columns<NV, E, TPR>(bias, 0.f, t, d, b);
-  for (int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / TPR; row < rows; row += (int64_t)gridDim.x * PER) {
+  Vec<T> next[NV];
+  const auto load = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) next[i].load(x + row * ldx + (i * TPR + t) * E, d - (i * TPR + t) * E);
+  };
+  int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
+  const int64_t step = (int64_t)gridDim.x * PER;
+  if (row < rows) load(row);
+  for (; row < rows; row += step) {
     Vec<T> v[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i].load(x + row * ldx + (i * TPR + t) * E, d - (i * TPR + t) * E);
+    for (int i = 0; i < NV; ++i) v[i] = next[i];
+    if (row + step < rows) load(row + step);             // (on its way while this row is worked on)
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < E; ++j) s += to_float(v[i].e[j]);
+      for (int j = 0; j < E; ++j) s += v[i].get(j);
     const float m = row_sum<TPR, BLOCK>(s, lds) / d;
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const float c = (i * TPR + t) * E + j < d ? to_float(v[i].e[j]) - m : 0.f;
-        s += c * c;
+        const float c = (i * TPR + t) * E + j < d ? v[i].get(j) - m : 0.f;
+        s = fmaf(c, c, s);
       }
     const float r = 1.f / sqrtf(row_sum<TPR, BLOCK>(s, lds) / d + eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      Vec<T> o;
+      float f[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) o.e[j] = from_float<T>((to_float(v[i].e[j]) - m) * r * w[i][j] + b[i][j]);
+      for (int j = 0; j < E; ++j) f[j] = fmaf((v[i].get(j) - m) * r, w[i][j], b[i][j]);
+      Vec<T> o;
+      o.put(f);
       o.store(y + row * ldy + (i * TPR + t) * E, d - (i * TPR + t) * E);
     }
     if (t == 0 && mean) { mean[row] = m; rstd[row] = r; }
@@ -142,37 +159,51 @@ __global__ void __launch_bounds__(BLOCK) k_norm_back(const int64_t* offsets, int
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < E; ++j) sw[i][j] = sb[i][j] = 0.f;
+  Vec<T> nx[NV], ny[NV];
+  float nm, nr;
+  const auto load = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      nx[i].load(x + row * ldx + (i * TPR + t) * E, d - (i * TPR + t) * E);
+      ny[i].load(dy + row * ldy + (i * TPR + t) * E, d - (i * TPR + t) * E);
+    }
+    nm = mean[row];
+    nr = rstd[row];
+  };
+  if (s.begin + sub < s.end) load(s.begin + sub);
   for (int64_t row = s.begin + sub; row < s.end; row += PER) {
     Vec<T> vx[NV], vy[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      vx[i].load(x + row * ldx + (i * TPR + t) * E, d - (i * TPR + t) * E);
-      vy[i].load(dy + row * ldy + (i * TPR + t) * E, d - (i * TPR + t) * E);
+      vx[i] = nx[i];
+      vy[i] = ny[i];
     }
-    const float m = mean[row], r = rstd[row];
+    const float m = nm, r = nr;
+    if (row + PER < s.end) load(row + PER);              // (on its way while this row is worked on)
     float a = 0.f, q = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const float g = to_float(vy[i].e[j]), h = (to_float(vx[i].e[j]) - m) * r;
+        const float g = vy[i].get(j), h = (vx[i].get(j) - m) * r;
         const float c = g * w[i][j];          // (0 behind the row's end, where g is)
         a += c;
-        q += c * h;
-        sw[i][j] += g * h;
+        q = fmaf(c, h, q);
+        sw[i][j] = fmaf(g, h, sw[i][j]);
         sb[i][j] += g;
       }
     row_sums<TPR, BLOCK>(a, q, lds);
-    a /= d;
-    q /= d;
+    a *= -r / d;
+    q *= -r / d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      Vec<T> o;
+      vx[i].again();
+      vy[i].again();
+      float f[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float h = (to_float(vx[i].e[j]) - m) * r;
-        o.e[j] = from_float<T>(r * (to_float(vy[i].e[j]) * w[i][j] - a - h * q));
-      }
+      for (int j = 0; j < E; ++j) f[j] = fmaf(vy[i].get(j) * w[i][j], r, fmaf((vx[i].get(j) - m) * r, q, a));
+      Vec<T> o;
+      o.put(f);
       o.store(dx + row * ldd + (i * TPR + t) * E, d - (i * TPR + t) * E);
     }
   }
@@ -284,27 +315,25 @@ __global__ void __launch_bounds__(1024) k_norm_join(const int64_t* offsets, int6
 constexpr int64_t kDropBlocks = 8192;
 constexpr int64_t kNormBlocks = 2048;      // eight to a compute unit; they go over the rows in turns
 
-// Rows of a slice: some 768 slices, three blocks to a compute unit, or as many as there are groups.
+// Rows of a slice: some 1024 slices, four blocks to a compute unit, or as many as there are groups.
 int slice_shift(int64_t rows) {
   int shift = 2;
-  while ((rows >> shift) > 768) ++shift;
+  while ((rows >> shift) > 1024) ++shift;
   return shift;
 }
 
-// f(threads of a row, vectors of a thread, threads of a block) for the least that hold d columns; false if `most` threads times
-// vectors do not.
-template <int E, int MOST, typename F>
+// f(threads of a row, vectors of a thread, threads of a block) for the least that hold d columns; false if none does.
+template <int E, typename F>
 bool by_width(int64_t d, F f) {
 #define ADACGD_WIDTH(TPR, NV, BLOCK)                                                                              \
-  if constexpr (TPR * NV <= MOST)                                                                                 \
-    if (d <= TPR * NV * E) { f(std::integral_constant<int, TPR>(), std::integral_constant<int, NV>(), std::integral_constant<int, BLOCK>()); return true; }
+  if (d <= TPR * NV * E) { f(std::integral_constant<int, TPR>(), std::integral_constant<int, NV>(), std::integral_constant<int, BLOCK>()); return true; }
+  ADACGD_WIDTH(16, 1, 256)
   ADACGD_WIDTH(64, 1, 256)
   ADACGD_WIDTH(64, 2, 256)
-  ADACGD_WIDTH(64, 4, 256)
+  ADACGD_WIDTH(256, 1, 256)
   ADACGD_WIDTH(256, 2, 256)
-  ADACGD_WIDTH(256, 4, 256)
+  ADACGD_WIDTH(1024, 1, 1024)
   ADACGD_WIDTH(1024, 2, 1024)
-  ADACGD_WIDTH(1024, 4, 1024)
 #undef ADACGD_WIDTH
   return false;
 }
@@ -340,14 +369,18 @@ __global__ void __launch_bounds__(256) k_dropout(const T* x, int64_t ldx, const 
       philox4x32_10((uint32_t)n, (uint32_t)(n >> 32), step, layer + 1, (uint32_t)seed, (uint32_t)(seed >> 32), w);
       if (whole) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t draw = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff;
-          float f = draw >= cut ? to_float(v[k / E].e[k % E]) * scale : 0.f;
-          if (residual) f += to_float(r[k / E].e[k % E]);
-          v[k / E].e[k % E] = from_float<T>(f);
-        }
+        for (int i = 0; i < V; ++i) {
+          float f[E];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i].store(o + c + i * E, E);
+          for (int j = 0; j < E; ++j) {
+            const int k = i * E + j;
+            const uint32_t draw = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff;
+            f[j] = draw >= cut ? v[i].get(j) * scale : 0.f;
+            if (residual) f[j] += r[i].get(j);
+          }
+          v[i].put(f);
+          v[i].store(o + c + i * E, E);
+        }
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -381,7 +414,7 @@ int adacgd_layer_norm(int64_t rows, int64_t d, const adacgd_tensor* x, const flo
   if (rows == 0) return ADACGD_OK;
   return by_dtype(x->dtype, [&](auto t) {
     using T = decltype(t);
-    const bool held = by_width<Vec<T>::kElems, sizeof(T) == 2 ? 2048 : 4096>(d, [&](auto tpr, auto nv, auto block) {
+    const bool held = by_width<Vec<T>::kElems>(d, [&](auto tpr, auto nv, auto block) {
       const int64_t blocks = (rows + block / tpr - 1) / (block / tpr);
       k_norm<T, tpr, nv, block><<<blocks < kNormBlocks ? blocks : kNormBlocks, block.value, 0, (hipStream_t)stream>>>(
           (const T*)x->data, x->stride, weight, bias, rows, (int)d, (float)eps, (T*)y->data, y->stride, mean, rstd);
@@ -430,7 +463,7 @@ int adacgd_layer_norm_backward(int64_t rows, int64_t groups, int64_t d, const in
   const int64_t numbers = slice_numbers(rows, groups, shift);
   return by_dtype(x->dtype, [&](auto t) -> int {
     using T = decltype(t);
-    const bool held = by_width<Vec<T>::kElems, 2048>(d, [&](auto tpr, auto nv, auto block) {
+    const bool held = by_width<Vec<T>::kElems>(d, [&](auto tpr, auto nv, auto block) {
       k_norm_back<T, tpr, nv, block><<<numbers, block.value, 0, (hipStream_t)stream>>>(offsets, groups, rows, (const T*)dy->data, dy->stride, (const T*)x->data, x->stride, weight,
                                                                                mean, rstd, (int)d, (T*)dx->data, dx->stride, out);
     });

@@ -6,62 +6,123 @@
 namespace adacgd {
 namespace {
 
+constexpr int64_t kMaxPairs = 1 << 22;      // (one launch takes 2^32 threads)
+constexpr float kLog2e = 1.4426950408889634f;
+
 struct Lse { float top, sum; };       // sum of exp(x - top)
 __device__ __forceinline__ Lse join(Lse a, Lse b) {
   const float top = fmaxf(a.top, b.top);
-  // (a part without elements has top = -inf and sum 0; infinities of the row give the NaN that the definition gives)
+  // (a part without elements, or of nothing but -inf, has sum 0; a row's other infinities give the NaN that the definition gives)
   const float fa = a.sum == 0.f ? 0.f : a.sum * expf(a.top - top), fb = b.sum == 0.f ? 0.f : b.sum * expf(b.top - top);
   return Lse{top, fa + fb};
 }
+// x - y is formed before the factor of the base: near the largest elements, which make up the sum, it has no error.
+__device__ __forceinline__ float exp_diff(float x, float y) { return __builtin_amdgcn_exp2f((x - y) * kLog2e); }
 
-// Largest element and sum of exponentials of every token's row that counts.
-template <typename T>
-__global__ void __launch_bounds__(256) k_token(int64_t tokens, int64_t sequences, int64_t v, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets, Lse* parts) {
+// A row is split into parts where there are few rows, so that 1024 blocks are at work; each part is whole vectors of a block.
+struct Parts {
+  int64_t count, length;
+};
+constexpr int kUnroll = 4;      // vectors of a thread on their way
+inline Parts parts_of(int64_t tokens, int64_t v) {
+  const int64_t unit = 2048;
+  int64_t count = tokens > 0 ? 1024 / tokens : 1;
+  const int64_t most = (v + unit - 1) / unit;
+  count = count < 1 ? 1 : count > most ? most : count;
+  const int64_t length = ((v + count - 1) / count + unit - 1) / unit * unit;
+  return Parts{(v + length - 1) / length, length};
+}
+inline bool narrow(int64_t v) { return v <= 8192; }      // a wavefront to a row, else 256 threads
+
+// Largest element and sum of exponentials of (a part of) every row that counts, in one pass: a thread's sum is scaled down
+// when one of its vectors has a larger element.  The target's logit is put aside by the part that has it.  Bound by memory where
+// a row is long; its exponentials take half of that time.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(256) k_token(int64_t tokens, int64_t sequences, int64_t v, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets,
+                                               Parts parts, Lse* out, float* at_target) {
+  constexpr int E = Vec<T>::kElems, PER = 256 / TPR;
   __shared__ Lse part[4];
-  const int64_t t = blockIdx.x;
-  if (t < offset_at(offsets, 0, tokens) || t >= offset_at(offsets, sequences, tokens)) return;
-  const int64_t target = targets[t];
-  if (target < 0 || target >= v) return;
-  logits += t * ld;
-  float top = -INFINITY;
-  for (int64_t c = threadIdx.x; c < v; c += 256) top = fmaxf(top, to_float(logits[c]));
-  float sum = 0.f;
-  const float base = top == -INFINITY ? 0.f : top;          // (a part of nothing but -inf sums to 0)
-  for (int64_t c = threadIdx.x; c < v; c += 256) sum += expf(to_float(logits[c]) - base);
-  Lse l{top, sum};
-  for (int o = 32; o > 0; o >>= 1) l = join(l, Lse{__shfl_xor(l.top, o, 64), __shfl_xor(l.sum, o, 64)});
-  if (lane_id() == 0) part[threadIdx.x / 64] = l;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 4; ++w) l = join(l, part[w]);
-    parts[t] = l;
+  const int t0 = threadIdx.x % TPR;
+  const int64_t first = offset_at(offsets, 0, tokens), last = offset_at(offsets, sequences, tokens);
+  for (int64_t u = (int64_t)blockIdx.x * PER + threadIdx.x / TPR; u < tokens * parts.count; u += (int64_t)gridDim.x * PER) {
+    const int64_t t = u / parts.count, begin = (u - t * parts.count) * parts.length;
+    if (t < first || t >= last) continue;
+    const int64_t target = targets[t];
+    if (target < 0 || target >= v) continue;
+    const int64_t end = begin + parts.length < v ? begin + parts.length : v;
+    const T* row = logits + t * ld;
+    if (t0 == 0 && target >= begin && target < end) at_target[t] = to_float(row[target]);
+    Lse l{-INFINITY, 0.f};
+    const auto take = [&](const Vec<T>& q) {
+      float top = q.get(0);
+#pragma unroll
+      for (int j = 1; j < E; ++j) top = fmaxf(top, q.get(j));
+      if (top > l.top) {
+        if (l.sum != 0.f) l.sum *= exp_diff(l.top, top);
+        l.top = top;
+      }
+      const float base = l.top == -INFINITY ? 0.f : l.top;
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < E; ++j) s += exp_diff(q.get(j), base);
+      l.sum += s;
+    };
+    int64_t c = begin + t0 * E;
+    for (; c + (kUnroll - 1) * TPR * E + E <= end; c += kUnroll * TPR * E) {
+      Vec<T> q[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) q[k].load(row + c + k * TPR * E, E);
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) take(q[k]);
+    }
+    for (; c < end; c += TPR * E) {
+      Vec<T> q;
+      q.load(row + c, end - c, -INFINITY);
+      take(q);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l = join(l, Lse{__shfl_xor(l.top, o, 64), __shfl_xor(l.sum, o, 64)});
+    if constexpr (TPR > 64) {
+      if (lane_id() == 0) part[threadIdx.x / 64] = l;
+      __syncthreads();
+      if (t0 == 0)
+        for (int w = 1; w < 4; ++w) l = join(l, part[w]);
+      __syncthreads();
+    }
+    if (t0 == 0) out[u] = l;
   }
 }
 
-// Log-probabilities of a pair's tokens, the sum of their differences from the reference, and the loss.
-template <typename T>
-__global__ void __launch_bounds__(64) k_pair(int64_t tokens, int64_t v, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets, const Lse* parts, const float* ref, double beta, double smoothing, float* loss, float* margin, float* logp, float* lse) {
+// Log-probabilities of a pair's tokens, the sums of their differences from the reference, and the loss.
+constexpr int kPairThreads = 512;
+__global__ void __launch_bounds__(kPairThreads) k_pair(int64_t tokens, int64_t v, const int64_t* targets, const int64_t* offsets, int64_t parts, const Lse* in, const float* at_target,
+                                                       const float* ref, double beta, double smoothing, float* loss, float* margin, float* logp, float* lse) {
+  __shared__ double sums[kPairThreads / 64];
   const int64_t p = blockIdx.x;
-  double m = 0;
-  for (int q = 0; q < 2; ++q) {
-    const int64_t first = offset_at(offsets, 2 * p + q, tokens), last = offset_at(offsets, 2 * p + q + 1, tokens);
-    double s = 0;
-    for (int64_t t = first + threadIdx.x; t < last; t += 64) {
-      const int64_t target = targets[t];
-      double lp = 0, l = 0;
-      if (target >= 0 && target < v) {
-        const double ls = log((double)parts[t].sum);
-        l = parts[t].top + ls;
-        lp = ((double)to_float(logits[t * ld + target]) - (double)parts[t].top) - ls;
-        s += lp - (ref ? (double)ref[t] : 0.0);
-      }
-      logp[t] = (float)lp;
-      lse[t] = (float)l;
+  const int64_t first = offset_at(offsets, 2 * p, tokens), middle = offset_at(offsets, 2 * p + 1, tokens), last = offset_at(offsets, 2 * p + 2, tokens);
+  double s = 0;
+#pragma unroll 2
+  for (int64_t t = first + threadIdx.x; t < last; t += kPairThreads) {
+    const int64_t target = targets[t];
+    double lp = 0, l = 0;
+    if (target >= 0 && target < v) {
+      Lse a = in[t * parts];
+      for (int64_t k = 1; k < parts; ++k) a = join(a, in[t * parts + k]);
+      const double ls = log((double)a.sum);
+      l = a.top + ls;
+      lp = ((double)at_target[t] - (double)a.top) - ls;
+      const double ratio = lp - (ref ? (double)ref[t] : 0.0);
+      s += t < middle ? ratio : -ratio;
     }
-    s = wave_sum(s);
-    m = q ? m - s : s;
+    logp[t] = (float)lp;
+    lse[t] = (float)l;
   }
+  s = wave_sum(s);
+  if (lane_id() == 0) sums[threadIdx.x / 64] = s;
+  __syncthreads();
   if (threadIdx.x == 0) {
+    double m = sums[0];
+    for (int w = 1; w < kPairThreads / 64; ++w) m += sums[w];
     const double z = beta * m, soft = log1p(exp(-fabs(z)));
     margin[p] = (float)m;
     // (a weight of zero takes its term away, an infinite one too)
@@ -69,32 +130,71 @@ __global__ void __launch_bounds__(64) k_pair(int64_t tokens, int64_t v, const T*
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequences, int64_t v, const float* dloss, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, T* out, int64_t ldo) {
-  const int64_t t = blockIdx.x;
-  if (t < offset_at(offsets, 0, tokens) || t >= offset_at(offsets, sequences, tokens)) return;
-  logits += t * ld;
-  out += t * ldo;
-  const int64_t target = targets[t];
-  if (target < 0 || target >= v) {
-    for (int64_t c = threadIdx.x; c < v; c += 256) out[c] = from_float<T>(0.f);
-    return;
-  }
-  int64_t low = 0, count = sequences;                 // the last sequence that begins at or before t
-  while (count > 1) { const int64_t h = count / 2; if (offset_at(offsets, low + h, tokens) <= t) { low += h; count -= h; } else count = h; }
-  const double z = beta * (double)margin[low / 2];
-  const double slope = (smoothing / (1 + exp(-z)) - (1 - smoothing) / (1 + exp(z))) * beta * (double)dloss[low / 2];
-  const float f = (float)(low % 2 ? -slope : slope);
-  const float l = lse[t];
-  for (int64_t c = threadIdx.x; c < v; c += 256) {
-    const float e = expf(to_float(logits[c]) - l);
-    out[c] = from_float<T>(f * ((c == target ? 1.f : 0.f) - e));
+// dlogits of (a part of) every row: f (onehot - exp(x - lse)), f from the margin of the row's pair.  Bound by memory.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequences, int64_t v, const float* dloss, const T* logits, int64_t ld, const int64_t* targets,
+                                                    const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, Parts parts, T* out, int64_t ldo) {
+  constexpr int E = Vec<T>::kElems, PER = 256 / TPR;
+  const int t0 = threadIdx.x % TPR, lane = (int)lane_id();
+  const int64_t first = offset_at(offsets, 0, tokens), last = offset_at(offsets, sequences, tokens);
+  for (int64_t u = (int64_t)blockIdx.x * PER + threadIdx.x / TPR; u < tokens * parts.count; u += (int64_t)gridDim.x * PER) {
+    const int64_t t = u / parts.count, begin = (u - t * parts.count) * parts.length;
+    if (t < first || t >= last) continue;
+    const int64_t end = begin + parts.length < v ? begin + parts.length : v;
+    const T* row = logits + t * ld;
+    T* o = out + t * ldo;
+    const int64_t target = targets[t];
+    if (target < 0 || target >= v) {
+      const Vec<T> zero{word4{0, 0, 0, 0}};
+      for (int64_t c = begin + t0 * E; c < end; c += TPR * E) zero.store(o + c, end - c);
+      continue;
+    }
+    // the last sequence that begins at or before t: 64 of them looked at with one load
+    int64_t low = 0, count = sequences;
+    while (count > 1) {
+      const int64_t step = (count + 63) / 64;
+      const bool here = lane * step < count;
+      const uint64_t m = ballot(here && offset_at(offsets, low + (here ? lane * step : 0), tokens) <= t);
+      const int64_t hit = m ? 63 - __builtin_clzll(m) : 0;
+      low += hit * step;
+      count = count - hit * step < step ? count - hit * step : step;
+    }
+    const double z = beta * (double)margin[low / 2];
+    const double slope = (smoothing / (1 + exp(-z)) - (1 - smoothing) / (1 + exp(z))) * beta * (double)dloss[low / 2];
+    const float f = (float)(low % 2 ? -slope : slope), l = lse[t];
+    const auto take = [&](Vec<T>& q, int64_t c) {
+      float g[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) g[j] = f * ((c + j == target ? 1.f : 0.f) - exp_diff(q.get(j), l));
+      q.put(g);
+    };
+    int64_t c = begin + t0 * E;
+    for (; c + (kUnroll - 1) * TPR * E + E <= end; c += kUnroll * TPR * E) {
+      Vec<T> q[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) q[k].load(row + c + k * TPR * E, E);
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        take(q[k], c + k * TPR * E);
+        q[k].store(o + c + k * TPR * E, E);
+      }
+    }
+    for (; c < end; c += TPR * E) {
+      Vec<T> q;
+      q.load(row + c, end - c);
+      take(q, c);
+      q.store(o + c, end - c);
+    }
   }
 }
+inline int64_t token_blocks(int64_t units) { return units < (int64_t(1) << 20) ? units : int64_t(1) << 20; }
+
+// Workspace: sums of the parts of rows, then the targets' logits.
+inline int64_t sums_bytes(int64_t tokens, int64_t v) { return (tokens * parts_of(tokens, v).count * (int64_t)sizeof(Lse) + 255) / 256 * 256; }
 
 int check_common(int64_t tokens, int64_t pairs, int64_t v, const adacgd_tensor* logits, const int64_t* targets, const int64_t* offsets, double beta, double smoothing) {
   ADACGD_TRY(check_count("tokens", tokens, 0, kMaxCount));
-  ADACGD_TRY(check_count("pairs", pairs, 0, kMaxCount / 2));
+  ADACGD_TRY(check_count("pairs", pairs, 0, kMaxPairs));
   ADACGD_TRY(check_count("v", v, 1, kMaxColumns));
   ADACGD_TRY(check_tensor(logits, "logits", tokens, v, false, false));
   if (tokens > 0 && !targets) return fail(ADACGD_ERR_ARG, "targets is null");
@@ -114,9 +214,9 @@ extern "C" {
 int adacgd_preference_loss_workspace_bytes(int64_t tokens, int64_t pairs, int64_t v, int64_t* bytes) {
   if (!bytes) return fail(ADACGD_ERR_ARG, "bytes is null");
   ADACGD_TRY(check_count("tokens", tokens, 0, kMaxCount));
-  ADACGD_TRY(check_count("pairs", pairs, 0, kMaxCount / 2));
+  ADACGD_TRY(check_count("pairs", pairs, 0, kMaxPairs));
   ADACGD_TRY(check_count("v", v, 1, kMaxColumns));
-  *bytes = (tokens * (int64_t)sizeof(Lse) + 255) / 256 * 256;
+  *bytes = sums_bytes(tokens, v) + (tokens * (int64_t)sizeof(float) + 255) / 256 * 256;
   return ADACGD_OK;
 }
 
@@ -132,11 +232,19 @@ int adacgd_preference_loss(int64_t tokens, int64_t pairs, int64_t v, const adacg
   if (pairs == 0) return ADACGD_OK;
   return by_dtype(logits->dtype, [&](auto t) -> int {
     using T = decltype(t);
+    const Parts parts = parts_of(tokens, v);
+    Lse* sums = (Lse*)workspace;
+    float* at_target = (float*)((char*)workspace + sums_bytes(tokens, v));
+    const int64_t units = tokens * parts.count;
+    const hipStream_t on = (hipStream_t)stream;
     if (tokens > 0) {
-      k_token<T><<<tokens, 256, 0, (hipStream_t)stream>>>(tokens, 2 * pairs, v, (const T*)logits->data, logits->stride, targets, offsets, (Lse*)workspace);
+      if (narrow(v))
+        k_token<T, 64><<<token_blocks((units + 3) / 4), 256, 0, on>>>(tokens, 2 * pairs, v, (const T*)logits->data, logits->stride, targets, offsets, parts, sums, at_target);
+      else
+        k_token<T, 256><<<token_blocks(units), 256, 0, on>>>(tokens, 2 * pairs, v, (const T*)logits->data, logits->stride, targets, offsets, parts, sums, at_target);
       ADACGD_TRY(launched("adacgd_preference_loss"));
     }
-    k_pair<T><<<pairs, 64, 0, (hipStream_t)stream>>>(tokens, v, (const T*)logits->data, logits->stride, targets, offsets, (const Lse*)workspace, ref, beta, smoothing, loss, margin, logp, lse);
+    k_pair<<<pairs, kPairThreads, 0, on>>>(tokens, v, targets, offsets, parts.count, sums, at_target, ref, beta, smoothing, loss, margin, logp, lse);
     return launched("adacgd_preference_loss");
   });
 }
@@ -151,7 +259,14 @@ int adacgd_preference_loss_backward(int64_t tokens, int64_t pairs, int64_t v, co
   if (!dloss || !margin || !lse) return fail(ADACGD_ERR_ARG, "dloss, margin or lse is null");
   return by_dtype(logits->dtype, [&](auto t) {
     using T = decltype(t);
-    k_token_grad<T><<<tokens, 256, 0, (hipStream_t)stream>>>(tokens, 2 * pairs, v, dloss, (const T*)logits->data, logits->stride, targets, offsets, margin, lse, beta, smoothing, (T*)dlogits->data, dlogits->stride);
+    const Parts parts = parts_of(tokens, v);
+    const int64_t units = tokens * parts.count;
+    const auto go = [&](auto kernel, int64_t blocks) {
+      kernel<<<token_blocks(blocks), 256, 0, (hipStream_t)stream>>>(tokens, 2 * pairs, v, dloss, (const T*)logits->data, logits->stride, targets, offsets, margin, lse, beta, smoothing,
+                                                                    parts, (T*)dlogits->data, dlogits->stride);
+    };
+    if (narrow(v)) go(k_token_grad<T, 64>, (units + 3) / 4);
+    else go(k_token_grad<T, 256>, units);
     return launched("adacgd_preference_loss_backward");
   });
 }
