@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(BLOCK) k_norm_back(const int64_t* offsets, int
       }
       __syncthreads();
       if (sub > 0) return;
-#pragma unroll
+#pragma unroll 1
       for (int u = 0; u < PER - 1; ++u)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -328,11 +328,12 @@ bool by_width(int64_t d, F f) {
 #define ADACGD_WIDTH(TPR, NV, BLOCK)                                                                              \
   if (d <= TPR * NV * E) { f(std::integral_constant<int, TPR>(), std::integral_constant<int, NV>(), std::integral_constant<int, BLOCK>()); return true; }
   ADACGD_WIDTH(16, 1, 256)
+  ADACGD_WIDTH(16, 2, 256)
   ADACGD_WIDTH(64, 1, 256)
   ADACGD_WIDTH(64, 2, 256)
   ADACGD_WIDTH(256, 1, 256)
   ADACGD_WIDTH(256, 2, 256)
-  ADACGD_WIDTH(1024, 1, 1024)
+  ADACGD_WIDTH(512, 2, 512)
   ADACGD_WIDTH(1024, 2, 1024)
 #undef ADACGD_WIDTH
   return false;
