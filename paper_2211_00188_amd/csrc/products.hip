@@ -13,6 +13,8 @@
 // Matrix instructions get B as first operand: a lane then holds four neighbouring columns of a row of C.
 // The order of the summed index inside an instruction does not matter as long as both operands agree on it: lane group q
 // (lane / 16) holds the q-th 16 bytes of a row's 64, eight elements of one instruction, or one element of each of four in fp32.
+#include <algorithm>
+
 #include "layers.h"
 
 namespace adacgd {
@@ -58,7 +60,7 @@ struct ProductArgs {
   const void* a;
   const void* b;
   void* c;
-  float* partial;                       // DW: slices' sums, where groups are cut
+  float* partial;                       // DW: sums of slices [numbers][n][k], where groups are cut; else null
   const int64_t* offsets;
   int64_t rows, groups, each;           // `each` entries of offsets to a group
   int64_t lda, ldb, ldc, gsb, gsc;
@@ -241,9 +243,10 @@ struct Tile {
   using LA = Loader<T, AT, BM, kWaves>;
   using LB = Loader<T, BT, BN, kWaves>;
   static constexpr int kStage = LA::kBytes + LB::kBytes;
-  static constexpr int kLds = 2 * kStage > kWaves * kStoreBytes * (int)sizeof(O) ? 2 * kStage : kWaves * kStoreBytes * (int)sizeof(O);
+  static constexpr int kLds = 2 * kStage > kWaves * kStoreBytes * 4 ? 2 * kStage : kWaves * kStoreBytes * 4;
 
-  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, int64_t ldc, char* lds) {
+  // (to `partial`, if that is not null, in fp32)
+  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, float* partial, int64_t ldc, char* lds) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const int m0 = wave / WN * (MI * 16), n0 = wave % WN * (NJ * 16);
     f32x4 acc[MI][NJ];
@@ -306,7 +309,8 @@ struct Tile {
     }
     static_assert(MI == 4 && NJ == 4, "");
     __syncthreads();                                                   // (the slabs have been read)
-    store<O>(acc, c + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
+    if (AT && partial) store<float>(acc, partial + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * 4, lane);
+    else store<O>(acc, c + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
   }
 };
 
@@ -329,7 +333,8 @@ struct Wide {
   using LB = Loader<T, BT, 256, 8>;
   static constexpr int kSlot = LA::kBytes, kSlots = 5, kLds = kSlots * kSlot;
 
-  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, int64_t ldc, char* lds) {
+  // (to `partial`, if that is not null, in fp32)
+  static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, float* partial, int64_t ldc, char* lds) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const int m0 = wave / 4 * 128, n0 = wave % 4 * 64;
     f32x4 acc[8][4];
@@ -394,9 +399,12 @@ struct Wide {
     }
     if (wave < 4) barrier();                                           // (and the slabs have been read)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      store<O>(reinterpret_cast<const f32x4(&)[4][4]>(acc[h * 4]), c + (m0 + h * 64) * ldc + n0, ldc, a.valid - m0 - h * 64, b.valid - n0,
-               lds + wave * kStoreBytes * sizeof(O), lane);
+    for (int h = 0; h < 2; ++h) {
+      const auto& half = reinterpret_cast<const f32x4(&)[4][4]>(acc[h * 4]);
+      const int64_t at = (m0 + h * 64) * ldc + n0;
+      if (AT && partial) store<float>(half, partial + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * kStoreBytes * 4, lane);
+      else store<O>(half, c + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
+    }
   }
 };
 
@@ -412,7 +420,7 @@ __global__ void __launch_bounds__(K::kThreads) k_rows_product(ProductArgs p) {
   const int64_t c0 = j * BN;
   const Operand a{(const char*)p.a + s.begin * p.lda * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(s.end - s.begin)};
   const Operand b{(const char*)p.b + (s.group * p.gsb + (BT ? c0 : c0 * p.ldb)) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(cols - c0)};
-  K::run(a, b, red, (O*)p.c + s.begin * p.ldc + c0, p.ldc, lds);
+  K::run(a, b, red, (O*)p.c + s.begin * p.ldc + c0, nullptr, p.ldc, lds);
 }
 
 template <typename T, typename O, typename K>
@@ -422,13 +430,102 @@ __global__ void __launch_bounds__(K::kThreads) k_group_product(ProductArgs p) {
   const int64_t tn = (p.n + BM - 1) / BM;
   int64_t i, j;
   if (!tile_of(blockIdx.x, p.patches, i, j)) return;
-  const int64_t g = i / tn, n0 = (i - g * tn) * BM, k0 = j * BN;
-  const int64_t first = offset_at(p.offsets, g, p.rows);
-  int64_t last = offset_at(p.offsets, g + 1, p.rows);
-  if (last < first) last = first;
-  const Operand a{(const char*)p.a + (first * p.lda + n0) * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(p.n - n0)};
-  const Operand b{(const char*)p.b + (first * p.ldb + k0) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(p.k - k0)};
-  K::run(a, b, last - first, (O*)p.c + g * p.gsc + n0 * p.ldc + k0, p.ldc, lds);
+  const int64_t number = i / tn, n0 = (i - number * tn) * BM, k0 = j * BN;
+  Slice s;
+  if (p.partial) {
+    s = find_slice(p.offsets, p.groups, p.rows, 1, p.shift, number);
+    if (s.group < 0) return;
+  } else {                                       // one slice to a group
+    s.group = number;
+    s.begin = s.first = offset_at(p.offsets, number, p.rows);
+    s.end = s.last = offset_at(p.offsets, number + 1, p.rows);
+    if (s.end < s.begin) s.end = s.last = s.begin;
+  }
+  const Operand a{(const char*)p.a + (s.begin * p.lda + n0) * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(p.n - n0)};
+  const Operand b{(const char*)p.b + (s.begin * p.ldb + k0) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(p.k - k0)};
+  if (p.partial && s.last - s.first > int64_t(1) << p.shift)
+    K::run(a, b, s.end - s.begin, nullptr, p.partial + (number * p.n + n0) * p.k + k0, p.k, lds);
+  else
+    K::run(a, b, s.end - s.begin, (O*)p.c + s.group * p.gsc + n0 * p.ldc + k0, nullptr, p.ldc, lds);
+}
+
+// Sums of the slices of every group that has several, in their order.
+template <typename O>
+__global__ void __launch_bounds__(256) k_join(ProductArgs p) {
+  const int64_t g = blockIdx.y;
+  const int64_t first = offset_at(p.offsets, g, p.rows), last = offset_at(p.offsets, g + 1, p.rows);
+  const int64_t count = (last - first + (int64_t(1) << p.shift) - 1) >> p.shift;
+  if (count <= 1) return;
+  const int64_t size = (int64_t)p.n * p.k, e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= size) return;
+  const float* from = p.partial + first_number(first, g, p.shift) * size + e;
+  const int64_t have = size - e;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int64_t j = 0; j < count; ++j) {
+    Vec<float> v;
+    v.load(from + j * size, have);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += v.get(q);
+  }
+  O* c = (O*)p.c + g * p.gsc;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q < have) c[(e + q) / p.k * p.ldc + (e + q) % p.k] = from_float<O>(sum[q]);
+}
+
+// FORWARD with few rows to a group (tokens served one by one): bound by reading the weights once.  A block has 16 rows of a group
+// and 16 of its columns; its WAVES wavefronts share the summed index, 128 bytes in turn, and read their fragments straight from memory --
+// nothing is used twice in a block, and without LDS slabs a wavefront has 8 lines of each of 16 rows on their way at once.  Their sums
+// are added up in LDS in order.  Lane group q takes bytes 32 q to 32 q + 31 of a line, so that each load asks for whole lines.
+template <typename T, typename O, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_few_rows(ProductArgs p) {
+  constexpr int kElem = 16 / sizeof(T), kLine = 128 / sizeof(T), U = 4;
+  __shared__ float sums[WAVES][16][17];
+  int64_t number, j;
+  if (!tile_of(blockIdx.x, p.patches, number, j)) return;
+  const Slice s = find_slice(p.offsets, p.groups, p.rows, p.each, p.shift, number);
+  if (s.group < 0 || s.end <= s.begin) return;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, l = lane & 15, q = lane >> 4;
+  const int n0 = (int)j * 16;
+  // rows and columns that do not exist are read as the last one that does, and not written
+  const int64_t row = s.begin + l < s.end ? s.begin + l : s.end - 1;
+  const int col = n0 + l < p.n ? n0 + l : p.n - 1;
+  const T* a = (const T*)p.a + row * p.lda;
+  const T* b = (const T*)p.b + s.group * p.gsb + (int64_t)col * p.ldb;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  int r = wave * kLine + q * 2 * kElem;
+  for (; r - q * 2 * kElem + (U - 1) * WAVES * kLine + kLine <= p.k; r += U * WAVES * kLine) {
+    word4 fa[2 * U], fb[2 * U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) __builtin_memcpy(&fb[2 * u + h], b + r + u * WAVES * kLine + h * kElem, 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) __builtin_memcpy(&fa[2 * u + h], a + r + u * WAVES * kLine + h * kElem, 16);
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u) acc = multiply(T(), fb[u], fa[u], acc);
+  }
+  for (; r - q * 2 * kElem < p.k; r += WAVES * kLine) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Vec<T> va, vb;
+      va.load(a + r + h * kElem, p.k - r - h * kElem);
+      vb.load(b + r + h * kElem, p.k - r - h * kElem);
+      acc = multiply(T(), vb.w, va.w, acc);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sums[wave][l][q * 4 + i] = acc[i];
+  __syncthreads();
+  if (threadIdx.x >= 256) return;
+  const int m = threadIdx.x / 16, n = threadIdx.x % 16;
+  float sum = sums[0][m][n];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) sum += sums[w][m][n];
+  if (s.begin + m < s.end && n0 + n < p.n) ((O*)p.c)[(s.begin + m) * p.ldc + n0 + n] = from_float<O>(sum);
 }
 
 int check_sizes(int32_t product, int64_t rows, int64_t groups, int64_t n, int64_t k) {
@@ -456,8 +553,11 @@ template <typename T, typename O, template <bool, bool> class K>
 int launch(int32_t product, ProductArgs p, hipStream_t stream) {
   constexpr int BM = K<true, true>::kRows, BN = K<true, true>::kColumns, threads = K<true, true>::kThreads, lds = K<true, true>::kLds;
   if (product == ADACGD_DW) {
-    p.patches = patches_of(p.groups * ((p.n + BM - 1) / BM), (p.k + BN - 1) / BN);
-    return enqueue(k_group_product<T, O, K<true, true>>, patch_blocks(p.patches), threads, lds, stream, p);
+    p.patches = patches_of((p.partial ? slice_numbers(p.rows, p.groups, p.shift) : p.groups) * ((p.n + BM - 1) / BM), (p.k + BN - 1) / BN);
+    ADACGD_TRY((enqueue(k_group_product<T, O, K<true, true>>, patch_blocks(p.patches), threads, lds, stream, p)));
+    if (!p.partial) return ADACGD_OK;
+    k_join<O><<<dim3(((int64_t)p.n * p.k + 1023) / 1024, p.groups), 256, 0, stream>>>(p);
+    return launched("adacgd_group_matmul");
   }
   p.shift = __builtin_ctz(BM);
   p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), ((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN);
@@ -466,11 +566,48 @@ int launch(int32_t product, ProductArgs p, hipStream_t stream) {
   return enqueue(k_rows_product<T, O, true, K<false, true>>, blocks, threads, lds, stream, p);
 }
 template <typename T, typename O>
+int launch_few(ProductArgs p, hipStream_t stream) {
+  p.shift = 4;
+  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), (p.n + 15) / 16);
+  const int64_t blocks = patch_blocks(p.patches);
+  // (sixteen wavefronts to a block where four would leave compute units without work)
+  if (p.patches.across * p.groups < 512) return enqueue(k_few_rows<T, O, 16>, blocks, 1024, 0, stream, p);
+  return enqueue(k_few_rows<T, O, 4>, blocks, 256, 0, stream, p);
+}
+template <typename T, typename O>
 struct Tiles {
   template <bool AT, bool BT> using Large = Wide<T, O, AT, BT>;
   template <bool AT, bool BT> using Direct = Tile<T, O, AT, BT, 128, 128, 2, 2, true>;
   template <bool AT, bool BT> using Staged = Tile<T, O, AT, BT, 128, 128, 2, 2, false>;
 };
+
+// What a call of these sizes is done with, if rows of all operands are `straight` (below).
+struct Choice {
+  bool few;             // 16 rows and columns to a block
+  bool large;           // tiles of 256 x 256 (16-bit types), one block to a compute unit; else 128 x 128, two
+  int64_t tiles;        // of all groups' C, by the groups' average size
+  int shift;            // DW: rows of a slice, 0: groups are not cut
+};
+inline Choice choose(int32_t product, int64_t size, int64_t rows, int64_t groups, int64_t n, int64_t k, bool direct) {
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const auto tiles = [&](int64_t t) {
+    if (product == ADACGD_DW) return groups * up(n, t) * up(k, t);
+    return groups * up(up(rows, groups), t) * up(product == ADACGD_FORWARD ? n : k, t);
+  };
+  Choice c;
+  c.few = product == ADACGD_FORWARD && rows <= 16 * groups;
+  c.large = size == 2 && direct && n >= 256 && k >= 256 && (product == ADACGD_DW ? tiles(256) >= 64 : rows >= 192 * groups && tiles(256) >= 192);
+  c.tiles = tiles(c.large ? 256 : 128);
+  c.shift = 0;
+  if (product == ADACGD_DW) {
+    // cut the groups where their tiles leave compute units idle, into slices of 256 rows at least
+    const int64_t mean = up(rows, groups);
+    const int64_t parts = std::min(up(c.large ? 256 : 512, c.tiles), mean / 256);
+    if (parts > 1)
+      for (c.shift = 8; (mean >> (c.shift + 1)) >= parts; ++c.shift) {}
+  }
+  return c;
+}
 
 // Rows begin on 16 bytes and are whole 16 bytes, and a tile's rows are less than 2^31 bytes apart.
 bool straight(const adacgd_tensor* t, int64_t rows, int64_t columns, bool grouped) {
@@ -491,6 +628,13 @@ int adacgd_group_matmul_workspace_bytes(int32_t product, int32_t dtype, int64_t 
   if (dtype < 0 || dtype > ADACGD_FP16) return fail(ADACGD_ERR_ARG, "unknown type %d", dtype);
   ADACGD_TRY(check_sizes(product, rows, groups, n, k));
   *bytes = 0;
+  if (product == ADACGD_DW) {
+    // (for either alignment of the operands: the tensors are not known here)
+    for (const bool direct : {false, true}) {
+      const int shift = choose(product, dtype_size(dtype), rows, groups, n, k, direct).shift;
+      if (shift) *bytes = std::max(*bytes, (slice_numbers(rows, groups, shift) * n * k * 4 + 255) / 256 * 256);
+    }
+  }
   return ADACGD_OK;
 }
 
@@ -512,13 +656,18 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
   ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, {}, (int)n, (int)k, 0};
   if (!dw && b->group_stride == 0) { p.each = groups; p.groups = 1; }      // one matrix for all: one group
   const bool direct = straight(a, rows, product == ADACGD_FORWARD ? k : n, false) && straight(b, dw ? rows : n, k, !dw);
-  const bool large = direct && rows / p.groups >= 256 && n >= 256 && k >= 256;
+  const Choice pick = choose(product, dtype_size(a->dtype), rows, p.groups, n, k, direct);
+  if (pick.shift) {
+    p.partial = (float*)workspace;
+    p.shift = pick.shift;
+  }
   return by_dtype(a->dtype, [&](auto t) {
     using T = decltype(t);
     const auto go = [&](auto o) {
       using O = decltype(o);
+      if (pick.few) return launch_few<T, O>(p, (hipStream_t)stream);
       if constexpr (sizeof(T) == 2) {
-        if (large) return launch<T, O, Tiles<T, O>::template Large>(product, p, (hipStream_t)stream);
+        if (pick.large) return launch<T, O, Tiles<T, O>::template Large>(product, p, (hipStream_t)stream);
       }
       if (direct) return launch<T, O, Tiles<T, O>::template Direct>(product, p, (hipStream_t)stream);
       return launch<T, O, Tiles<T, O>::template Staged>(product, p, (hipStream_t)stream);
