@@ -7,7 +7,7 @@ namespace adacgd {
 namespace {
 
 constexpr int64_t kMaxPairs = 1 << 22;      // (one launch takes 2^32 threads)
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500929e-8f;      // log2(e) and what the first leaves of it
 
 struct Lse { float top, sum; };       // sum of exp(x - top)
 __device__ __forceinline__ Lse join(Lse a, Lse b) {
@@ -16,8 +16,13 @@ __device__ __forceinline__ Lse join(Lse a, Lse b) {
   const float fa = a.sum == 0.f ? 0.f : a.sum * expf(a.top - top), fb = b.sum == 0.f ? 0.f : b.sum * expf(b.top - top);
   return Lse{top, fa + fb};
 }
-// x - y is formed before the factor of the base: near the largest elements, which make up the sum, it has no error.
-__device__ __forceinline__ float exp_diff(float x, float y) { return __builtin_amdgcn_exp2f((x - y) * kLog2e); }
+// exp(x - y) by the instruction for powers of two.  x - y is formed before the factor of the base: near the largest elements, which
+// make up the sum, it has no error.  The factor's own rounding (1.3e-8 of it) would make every term too large: sums were off by
+// 5e-8 on average, and a pair's margin by that times the difference of its sequences' lengths.
+__device__ __forceinline__ float exp_diff(float x, float y) {
+  const float d = x - y;
+  return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eLow));
+}
 
 // A row is split into parts where there are few rows, so that 1024 blocks are at work; each part is whole vectors of a block.
 struct Parts {
