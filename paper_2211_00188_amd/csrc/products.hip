@@ -31,30 +31,36 @@ constexpr int kSlab = 128;      // bytes of the summed index
 // Blocks go to the eight dies in turn.  Tiles are dealt to the dies in patches of 32, one for each compute unit of a die, so that
 // those at work on a die at one time share rows and columns in its cache; patches, not long runs of tiles, so that each die
 // gets its share of the numbers that no slice has and of long groups.  A patch is 1 << lw tiles wide: 4 x 8, or as the
-// matrix allows.
+// matrix allows.  Patches are smaller (down to 4 tiles) where a group has fewer than eight of 32: a long group is every die's.
 struct Patches {
   int64_t down, across;
-  int lw;
+  int lp, lw;           // logarithms of a patch's tiles and of its width
 };
-inline Patches patches_of(int64_t down, int64_t across) {
-  int lw = 3;
+inline Patches patches_of(int64_t down, int64_t across, int64_t of_group) {
+  int lp = 5;
+  while (lp > 2 && of_group >> lp < 8) --lp;
+  int lw = (lp + 1) / 2;
   while (lw > 0 && int64_t(1) << (lw - 1) >= across) --lw;
-  while (lw < 5 && int64_t(1) << (5 - lw - 1) >= down) ++lw;
-  return Patches{down, across, lw};
+  while (lw < lp && int64_t(1) << (lp - lw - 1) >= down) ++lw;
+  return Patches{down, across, lp, lw};
 }
 __host__ __device__ inline int64_t patch_columns(const Patches& p) { return (p.across + (1 << p.lw) - 1) >> p.lw; }
 inline int64_t patch_blocks(const Patches& p) {
-  const int64_t rows = (p.down + (32 >> p.lw) - 1) / (32 >> p.lw);
-  return (rows * patch_columns(p) + 7) / 8 * 8 * 32;
+  const int64_t rows = (p.down + (1 << (p.lp - p.lw)) - 1) >> (p.lp - p.lw);
+  return ((rows * patch_columns(p) + 7) / 8 * 8) << p.lp;
 }
 __device__ __forceinline__ bool tile_of(uint32_t block, const Patches& p, int64_t& i, int64_t& j) {
   const uint32_t columns = (uint32_t)patch_columns(p);
-  const uint32_t patch = (block >> 8) * 8 + (block & 7), in = block >> 3 & 31;
+  const uint32_t patch = (block >> (3 + p.lp)) * 8 + (block & 7), in = block >> 3 & ((1u << p.lp) - 1);
   const uint32_t row = patch / columns;
-  i = (int64_t)row * (32 >> p.lw) + (in >> p.lw);
+  i = ((int64_t)row << (p.lp - p.lw)) + (in >> p.lw);
   j = ((int64_t)(patch - row * columns) << p.lw) + (in & ((1u << p.lw) - 1));
   return i < p.down && j < p.across;
 }
+
+// Where one load of a wavefront shows all groups, the slices that exist are counted instead: every die gets an eighth of the
+// tiles, down bands of four slices.  (16 groups of 1024 rows, 2048 columns: 20 patches for 8 dies took 305 us, this takes 225.)
+constexpr int kCounted = 64;
 
 struct ProductArgs {
   const void* a;
@@ -67,6 +73,32 @@ struct ProductArgs {
   Patches patches;
   int n, k, shift;
 };
+
+// The block's tile among those of slices that exist, of at most 64 groups.
+__device__ __forceinline__ bool find_tile(const ProductArgs& p, Slice& s, int64_t& j) {
+  const int lane = (int)lane_id();
+  uint32_t o = 0, end = 0;
+  if (lane < p.groups) {
+    o = (uint32_t)offset_at(p.offsets, lane * p.each, p.rows);
+    end = (uint32_t)offset_at(p.offsets, (lane + 1) * p.each, p.rows);
+    if (end < o) end = o;
+  }
+  const uint32_t count = (uint32_t)(((uint64_t)(end - o) + (1u << p.shift) - 1) >> p.shift);
+  const uint32_t upto = wave_scan(count), slices = lane_value(upto, 63), across = (uint32_t)p.patches.across;
+  const uint32_t total = slices * across, per = (total + 7) / 8, t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per || t >= total) return false;
+  const uint32_t band = t / (4 * across), rest = t - band * 4 * across, height = slices - band * 4 < 4 ? slices - band * 4 : 4;
+  const uint32_t i = band * 4 + rest % height;
+  j = rest / height;
+  const int g = (int)popc64(ballot(upto <= i));                 // groups whose slices all come before
+  if (g >= p.groups) return false;                              // (offsets that break the rule)
+  s.group = g;
+  s.first = lane_value(o, g);
+  s.last = lane_value(end, g);
+  s.begin = s.first + ((int64_t)(i - (lane_value(upto, g) - lane_value(count, g))) << p.shift);
+  s.end = s.begin + (int64_t(1) << p.shift) < s.last ? s.begin + (int64_t(1) << p.shift) : s.last;
+  return true;
+}
 
 // One operand of a tile: `valid` of the tile's rows (along) or columns (across) exist.
 struct Operand {
@@ -413,10 +445,16 @@ __global__ void __launch_bounds__(K::kThreads) k_rows_product(ProductArgs p) {
   constexpr int BN = K::kColumns;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int cols = BT ? p.k : p.n, red = BT ? p.n : p.k;
-  int64_t number, j;
-  if (!tile_of(blockIdx.x, p.patches, number, j)) return;
-  const Slice s = find_slice(p.offsets, p.groups, p.rows, p.each, p.shift, number);
-  if (s.group < 0 || s.end <= s.begin) return;
+  int64_t j;
+  Slice s;
+  if (p.groups <= kCounted) {
+    if (!find_tile(p, s, j)) return;
+  } else {
+    int64_t number;
+    if (!tile_of(blockIdx.x, p.patches, number, j)) return;
+    s = find_slice(p.offsets, p.groups, p.rows, p.each, p.shift, number);
+    if (s.group < 0 || s.end <= s.begin) return;
+  }
   const int64_t c0 = j * BN;
   const Operand a{(const char*)p.a + s.begin * p.lda * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(s.end - s.begin)};
   const Operand b{(const char*)p.b + (s.group * p.gsb + (BT ? c0 : c0 * p.ldb)) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(cols - c0)};
@@ -553,14 +591,15 @@ template <typename T, typename O, template <bool, bool> class K>
 int launch(int32_t product, ProductArgs p, hipStream_t stream) {
   constexpr int BM = K<true, true>::kRows, BN = K<true, true>::kColumns, threads = K<true, true>::kThreads, lds = K<true, true>::kLds;
   if (product == ADACGD_DW) {
-    p.patches = patches_of((p.partial ? slice_numbers(p.rows, p.groups, p.shift) : p.groups) * ((p.n + BM - 1) / BM), (p.k + BN - 1) / BN);
+    const int64_t tn = (p.n + BM - 1) / BM, tk = (p.k + BN - 1) / BN;
+    p.patches = patches_of((p.partial ? slice_numbers(p.rows, p.groups, p.shift) : p.groups) * tn, tk, tn * tk);
     ADACGD_TRY((enqueue(k_group_product<T, O, K<true, true>>, patch_blocks(p.patches), threads, lds, stream, p)));
     if (!p.partial) return ADACGD_OK;
     k_join<O><<<dim3(((int64_t)p.n * p.k + 1023) / 1024, p.groups), 256, 0, stream>>>(p);
     return launched("adacgd_group_matmul");
   }
   p.shift = __builtin_ctz(BM);
-  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), ((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN);
+  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), ((product == ADACGD_FORWARD ? p.n : p.k) + BN - 1) / BN, 256);
   const int64_t blocks = patch_blocks(p.patches);
   if (product == ADACGD_FORWARD) return enqueue(k_rows_product<T, O, false, K<false, false>>, blocks, threads, lds, stream, p);
   return enqueue(k_rows_product<T, O, true, K<false, true>>, blocks, threads, lds, stream, p);
@@ -568,7 +607,7 @@ int launch(int32_t product, ProductArgs p, hipStream_t stream) {
 template <typename T, typename O>
 int launch_few(ProductArgs p, hipStream_t stream) {
   p.shift = 4;
-  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), (p.n + 15) / 16);
+  p.patches = patches_of(slice_numbers(p.rows, p.groups, p.shift), (p.n + 15) / 16, 256);
   const int64_t blocks = patch_blocks(p.patches);
   // (sixteen wavefronts to a block where four would leave compute units without work)
   if (p.patches.across * p.groups < 512) return enqueue(k_few_rows<T, O, 16>, blocks, 1024, 0, stream, p);

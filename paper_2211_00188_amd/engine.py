@@ -322,6 +322,15 @@ class AdaCGD:
             return self._get(field, (2, len(KERNELS)), f64)
         raise ValueError(field)
 
+    def state_into(self, field, out):
+        """Copies a field into a GPU tensor of its type and size (no copy through the host)."""
+        assert out.is_cuda and out.is_contiguous()
+        lib = load_library()
+        rc = lib.adacgd_state(self.ctx, int(field), C.c_void_p(out.data_ptr()), out.numel() * out.element_size(), 1)
+        if rc:
+            raise AdaCGDError(rc, lib.adacgd_last_error(self.ctx).decode())
+        return out
+
     CHECKPOINT_FIELDS = (F_X, F_G, F_GTILDE, F_GTILDE_PREV, F_GI, F_PREV_GRAD, F_STEP, F_LEVEL_HIST, F_M_LEVEL_HIST)
 
     def set_state(self, field, array):

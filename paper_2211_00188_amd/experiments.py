@@ -7,6 +7,10 @@ All methods are special cases of the AdaCGD compressor (Section 4.3): one level 
 zeta = 0 = EF21, the identity level = LAG / GD, and run through the same engine.  The master
 compressor is the identity here, as in the paper's experiments.
 
+`--workload preference` runs the methods on a model whose gradients the engine is given: a norm, a residual
+block with dropout and a head under a preference loss, each worker's gradient from its own pairs
+(`preference_gradients`, by the operators of `layers.py`).
+
 The datasets of the paper are not available; the seeded synthetic stand-ins of
 `workloads.py` take their place.  The smoothness constants are computed on the host with
 NumPy; every step of the method itself runs on the GPU.
@@ -140,6 +144,86 @@ def run(wl, method, multiplier, bit_budget, max_steps=100000, zeta=1.0, chunk=50
     return np.array(steps), np.array(bits), np.array(gn)
 
 
+class PreferenceModel:
+    """A PreferenceWorkload on the GPU: logits = head (dropout(relu(hidden z)) + z), z = norm(features)."""
+
+    def __init__(self, wl, seed=0):
+        import torch
+        put = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+        self.wl, self.seed = wl, seed
+        self.features, self.targets, self.ref = put(wl.features), put(wl.targets), put(wl.ref)
+        self.sequences, self.rows = put(wl.sequences), put(wl.worker_rows())
+        counts = np.diff(wl.worker_pairs)
+        self.share = put((1.0 / np.repeat(counts, counts)).astype(np.float32))       # f_i: the mean over worker i's pairs
+
+    def gradients(self, x, step, ext):
+        """Gradients of every worker's f_i at x [d] into ext [n, d], each parameter's where it lies in the vector; returns the
+        pairs' losses.  Dropout draws anew for every step; all workers see the same parameters."""
+        from . import layers as L
+        wl, n = self.wl, self.wl.n
+        w, g = wl.parts(x), wl.parts(ext)
+        hidden, head = w["hidden"].expand(n, -1, -1), w["head"].expand(n, -1, -1)
+        drop = dict(p=wl.dropout, seed=self.seed, step=step)
+        z, mean, rstd = L.layer_norm(self.features, w["norm_weight"], w["norm_bias"])
+        u = L.group_matmul(z, hidden, self.rows)
+        s = L.dropout(u.clamp(min=0), residual=z, **drop)
+        logits = L.group_matmul(s, head, self.rows)
+        loss, margin, logp, lse = L.preference_loss(logits, self.targets, self.sequences, self.ref, wl.beta)
+        dlogits = L.preference_loss_backward(self.share, logits, self.targets, self.sequences, margin, lse, wl.beta, out=logits)
+        L.group_matmul_dw(dlogits, s, self.rows, out=g["head"])
+        ds = L.group_matmul_dx(dlogits, head, self.rows)
+        du = L.dropout(ds, **drop).mul_(u > 0)
+        L.group_matmul_dw(du, z, self.rows, out=g["hidden"])
+        dz = L.group_matmul_dx(du, hidden, self.rows).add_(ds)
+        L.layer_norm_backward(dz, self.features, w["norm_weight"], mean, rstd, self.rows, dweight=g["norm_weight"], dbias=g["norm_bias"])
+        return loss
+
+
+def run_preference(wl, method, gamma, bit_budget, max_steps=100000, zeta=1.0, seed=0):
+    """One method on a PreferenceWorkload until the uplink cost reaches `bit_budget` bits per worker: (steps, bits per worker,
+    ||mean gradient||^2, mean loss) after every step."""
+    import torch
+    from . import engine as E
+    levels, z = method_levels(method, wl.d, zeta=zeta)
+    model = PreferenceModel(wl, seed)
+    x = torch.from_numpy(wl.x0).cuda()
+    ext = torch.empty((wl.n, wl.d), device="cuda")
+    record = []
+
+    def note(t, bits, loss):
+        m = ext.double().mean(0)
+        record.append((t, bits, float(m @ m), float(loss.double().mean())))
+    loss = model.gradients(x, 0, ext)
+    eng = E.AdaCGD(n=wl.n, d=wl.d, gamma=gamma, worker_levels=levels, zeta_worker=z, grad_mode=E.GRAD_EXTERNAL, x0=x, grad0=ext)
+    g = torch.empty_like(x)
+    note(0, 0.0, loss)
+    while record[-1][0] < max_steps and record[-1][1] < bit_budget and np.isfinite(record[-1][2]):
+        t = record[-1][0] + 1
+        # the engine moves x by its g, rounded once, before it reads the gradients, which are those at the new x
+        x = (eng.state_into(E.F_X, x).double() - float(np.float32(gamma)) * eng.state_into(E.F_G, g).double()).float()
+        loss = model.gradients(x, t, ext)
+        eng.step(ext)
+        note(t, float(eng.state(E.F_COMM)[1]) / wl.n, loss)
+    eng.close()
+    return tuple(np.array(c) for c in zip(*record))
+
+
+def sweep_preference(wl, methods=METHODS, multipliers=tuple(2 ** k for k in range(9)), bit_budget=2e6, smoothness=16.0, **kw):
+    """For every method: the multiple of its theoretical stepsize, with an assumed smoothness constant, that reaches the lowest mean
+    loss within the budget."""
+    out = {}
+    for m in methods:
+        levels, z = method_levels(m, wl.d, zeta=kw.get("zeta", 1.0))
+        base_gamma = theoretical_stepsize(smoothness, smoothness, *three_pc_constants(m, [k / wl.d for _, k in levels], z))
+        for mult in multipliers:
+            s, b, gn, loss = run_preference(wl, m, base_gamma * mult, bit_budget, **kw)
+            final = float(loss[-1]) if np.isfinite(gn[-1]) else float("inf")
+            if m not in out or final < out[m]["loss"]:
+                out[m] = {"multiplier": mult, "loss": final, "grad_norm_sq": float(gn[-1]), "steps": int(s[-1]), "bits_per_worker": float(b[-1]),
+                          "gamma": base_gamma * mult, "curve": (s, b, gn)}
+    return out
+
+
 def sweep(wl, methods=METHODS, multipliers=tuple(2 ** k for k in range(9)), bit_budget=2e6, **kw):
     """For every method: the multiplier that reaches the lowest gradient norm within the budget."""
     Lm, Lp = smoothness_constants(wl)
@@ -161,20 +245,21 @@ def sweep(wl, methods=METHODS, multipliers=tuple(2 ** k for k in range(9)), bit_
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--workload", choices=["tiny", "sparse_logreg"], default="sparse_logreg")
+    ap.add_argument("--workload", choices=["tiny", "sparse_logreg", "preference"], default="sparse_logreg")
     ap.add_argument("--budget-bits", type=float, default=2e6, help="uplink bits per worker at which a run stops")
     ap.add_argument("--max-multiplier-log2", type=int, default=8)
     ap.add_argument("--zeta", type=float, default=1.0)
     ap.add_argument("--curves", metavar="FILE", help="write the best run of every method as CSV rows "
                     "method,step,bits_per_worker,grad_norm_sq (the axes of the paper's figures)")
     args = ap.parse_args()
-    wl = W.tiny() if args.workload == "tiny" else W.sparse_logreg()
-    res = sweep(wl, multipliers=tuple(2 ** k for k in range(args.max_multiplier_log2 + 1)),
+    wl = {"tiny": W.tiny, "sparse_logreg": W.sparse_logreg, "preference": W.preference}[args.workload]()
+    run_all = sweep_preference if args.workload == "preference" else sweep
+    res = run_all(wl, multipliers=tuple(2 ** k for k in range(args.max_multiplier_log2 + 1)),
                 bit_budget=args.budget_bits, zeta=args.zeta)
-    print("%-8s %10s %12s %10s %16s %14s" % ("method", "multiplier", "gamma", "steps", "bits/worker", "|grad f|^2"))
+    print("%-8s %10s %12s %10s %16s %14s" % ("method", "multiplier", "gamma", "steps", "bits/worker", "|grad f|^2") + (" %12s" % "mean loss" if args.workload == "preference" else ""))
     for m, r in res.items():
         print("%-8s %10d %12.4g %10d %16.4g %14.6g" % (m, r["multiplier"], r["gamma"], r["steps"],
-                                                     r["bits_per_worker"], r["grad_norm_sq"]))
+                                                     r["bits_per_worker"], r["grad_norm_sq"]) + (" %12.6g" % r["loss"] if "loss" in r else ""))
     if args.curves:
         with open(args.curves, "w") as f:
             f.write("method,step,bits_per_worker,grad_norm_sq\n")

@@ -61,6 +61,44 @@ class VectorWorkload:
     seed: int
 
 
+@dataclass
+class PreferenceWorkload:
+    """Pairs of token sequences split over workers; the model's parameters are one vector (see `parts`)."""
+    name: str
+    n: int
+    width: int                 # features of a token
+    vocab: int
+    features: np.ndarray       # [tokens, width] float32
+    targets: np.ndarray        # [tokens] int64, -100 where a token does not count
+    sequences: np.ndarray      # [2 pairs + 1] int64: token rows; sequence 2p is the preferred one of pair p
+    worker_pairs: np.ndarray   # [n+1] int64: pairs of worker i are [off[i], off[i+1])
+    ref: np.ndarray            # [tokens] float32: log-probabilities under the model that training starts from
+    x0: np.ndarray             # [d] float32
+    beta: float
+    dropout: float
+
+    @property
+    def d(self):
+        return sum(int(np.prod(shape)) for shape in self.shapes().values())
+
+    def shapes(self):
+        """Parameters in their order in the vector."""
+        return {"norm_weight": (self.width,), "norm_bias": (self.width,), "hidden": (self.width, self.width), "head": (self.vocab, self.width)}
+
+    def parts(self, x):
+        """Views of the last dimension of x (an array or tensor [..., d]) as the parameters."""
+        out, at = {}, 0
+        for name, shape in self.shapes().items():
+            size = int(np.prod(shape))
+            out[name] = x[..., at:at + size].reshape(tuple(x.shape[:-1]) + shape)
+            at += size
+        return out
+
+    def worker_rows(self):
+        """[n+1] int64: token rows of each worker."""
+        return self.sequences[2 * self.worker_pairs]
+
+
 def ratio_K(ratio: float, d: int) -> int:
     """K for a level given as a fraction of d: the ceiling, at least 1."""
     return max(1, min(d, math.ceil(ratio * d - 1e-9)))
@@ -244,3 +282,27 @@ class ModelSizedGrads:
         xi = self.rng.standard_normal(self.wl.d, dtype=np.float32)
         self.z = (np.float32(self.rho) * self.z + np.float32(math.sqrt(1 - self.rho ** 2)) * xi).astype(np.float32)
         return out
+
+
+def preference(n: int = 16, pairs: int = 128, width: int = 64, vocab: int = 250, length: int = 24, beta: float = 0.5, dropout: float = 0.1,
+               seed: int = 23) -> PreferenceWorkload:
+    """Preference pairs for a model of one residual block: token features are drawn, the preferred sequence's targets come from a
+    planted table of the vocabulary more often than the other's, lengths and shards differ, and a prompt at the head of every
+    sequence does not count."""
+    rng = _rng(seed)
+    cuts = np.sort(rng.choice(np.arange(1, pairs), n - 1, replace=False)) if n > 1 else np.array([], dtype=np.int64)
+    worker_pairs = np.concatenate([[0], cuts, [pairs]]).astype(np.int64)
+    lengths = rng.integers(max(2, length // 2), length + length // 2 + 1, 2 * pairs)
+    sequences = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    tokens = int(sequences[-1])
+    features = rng.standard_normal((tokens, width)).astype(np.float32)
+    planted = rng.standard_normal((vocab, width))
+    best = np.argmax(features.astype(np.float64) @ planted.T, axis=1)
+    preferred = np.repeat(np.arange(2 * pairs) % 2 == 0, lengths)
+    targets = np.where(rng.random(tokens) < np.where(preferred, 0.5, 0.1), best, rng.integers(0, vocab, tokens)).astype(np.int64)
+    position = np.arange(tokens) - np.repeat(sequences[:-1], lengths)
+    targets[position < np.repeat(lengths // 4, lengths)] = -100
+    x0 = np.concatenate([np.ones(width), np.zeros(width), rng.standard_normal(width * width) / math.sqrt(width),
+                         rng.standard_normal(vocab * width) * (0.3 / math.sqrt(width))]).astype(np.float32)
+    ref = np.full(tokens, -math.log(vocab), dtype=np.float32)
+    return PreferenceWorkload("preference", n, width, vocab, features, targets, sequences, worker_pairs, ref, x0, beta, dropout)

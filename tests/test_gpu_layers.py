@@ -601,6 +601,50 @@ def test_rows_more_than_four_gigabytes_apart():
     assert all(torch.equal(a, b) for a, b in zip(L.layer_norm_backward(far, far, None, mean, rstd, off)[1:], L.layer_norm_backward(near, near, None, mean, rstd, off)[1:]))
 
 
+def test_a_models_gradients_by_worker_and_the_engine_that_takes_them():
+    """Every operator in its place: each worker's gradient of a norm, a residual block with dropout and a head under the preference
+    loss, against automatic differentiation of that worker's own objective in 64 bits; then the engine's steps on them."""
+    from paper_2211_00188_amd import experiments as X
+    from paper_2211_00188_amd import workloads as W
+    wl = W.preference(n=4, pairs=10, width=16, vocab=33, length=14, seed=5)
+    model, step = X.PreferenceModel(wl, seed=3), 6
+    ext = torch.full((wl.n, wl.d), float("nan"), device="cuda")
+    loss = model.gradients(torch.from_numpy(wl.x0).cuda(), step, ext).cpu().double()
+    keep = torch.from_numpy(draws(wl.features.size, 3, step, 0, 0) >= math.floor(wl.dropout * 65536 + 0.5)).view(wl.features.shape)
+    scale = 65536 / (65536 - math.floor(wl.dropout * 65536 + 0.5))
+    f, t, rows = torch.from_numpy(wl.features).double(), torch.from_numpy(wl.targets), wl.worker_rows()
+    for i in range(wl.n):
+        x = torch.from_numpy(wl.x0).double().requires_grad_()
+        w = wl.parts(x)
+        z = norm64(f, w["norm_weight"], w["norm_bias"], 1e-5)[0]
+        u = z @ w["hidden"].t()
+        assert u.abs().min() > 1e-5                             # (no element so near the kink that fp32 might pass it)
+        logits = (u.clamp(min=0) * keep * scale + z) @ w["head"].t()
+        lp = logits.log_softmax(1)
+        counts = t >= 0
+        ratio = torch.where(counts, lp.gather(1, t.clamp(min=0)[:, None])[:, 0] - torch.from_numpy(wl.ref).double(), 0.0)
+        a, b = wl.worker_pairs[i:i + 2]
+        s = wl.sequences
+        margin = torch.stack([ratio[s[2 * p]:s[2 * p + 1]].sum() - ratio[s[2 * p + 1]:s[2 * p + 2]].sum() for p in range(a, b)])
+        each = torch.nn.functional.softplus(-wl.beta * margin)
+        assert (loss[a:b] - each.detach()).abs().max() < 1e-5
+        each.mean().backward()
+        for name, got in wl.parts(ext[i].cpu().double()).items():
+            want = wl.parts(x.grad)[name]
+            # a dozen operations one after the other, sums of some 40 to 140 terms in each: 12 * 140 u = 1e-4 of the largest
+            assert (got - want).abs().max() <= 1e-4 * want.abs().max(), (i, name)
+    levels, zeta = X.method_levels("adacgd", wl.d)
+    x0 = torch.from_numpy(wl.x0).cuda()
+    eng = E.AdaCGD(n=wl.n, d=wl.d, gamma=0.05, worker_levels=levels, zeta_worker=zeta, grad_mode=E.GRAD_EXTERNAL, x0=x0, grad0=ext)
+    eng.step(ext)
+    assert np.array_equal(eng.state(E.F_PREV_GRAD), ext.cpu().numpy())
+    out = torch.empty(wl.d, device="cuda")
+    assert np.array_equal(eng.state_into(E.F_X, out).cpu().numpy(), eng.state(E.F_X))
+    eng.close()
+    steps, bits, gn, mean_loss = X.run_preference(wl, "adacgd", 0.05, 2e4, max_steps=6)
+    assert len(steps) > 2 and np.isfinite(gn).all() and np.isfinite(mean_loss).all() and (np.diff(bits) >= 0).all()
+
+
 def test_the_binding_refuses_what_does_not_fit():
     x, w, off = torch.zeros((8, 16), device="cuda"), torch.zeros((2, 4, 16), device="cuda"), offsets_of([3, 5])
     for call in (lambda: L.group_matmul(x, w[:, :, :8], off), lambda: L.group_matmul(x, w[:1], off), lambda: L.group_matmul(x.t(), w, off),
