@@ -127,12 +127,13 @@ struct Loader {
   static constexpr int kRow = ACROSS ? R * (int)sizeof(T) : kSlab;        // bytes of a row in LDS
   static constexpr int kLoads = R * kSlab / 1024 / W;                     // of 16 bytes a lane
   static constexpr int kBytes = R * kSlab;
-  static_assert(kLoads * 1024 * W == kBytes, "");
+  static_assert(kLoads * 1024 * W == kBytes && kRow >= 128, "");      // (pieces are turned inside a row)
 
   // where pieces of row `k` are put, in chunks
   static __device__ __forceinline__ int turn(int k) {
     if (!ACROSS) return (k >> 1 & 1) * 2 + (k >> 3 & 1) * 4;
-    return sizeof(T) == 2 ? ((k & 3) + ((k >> 3 & 1) << 2)) << 1 : (k >> 2 & 3) << 2;
+    if (sizeof(T) == 4) return (k >> 2 & 3) << 2;
+    return kRow >= 256 ? ((k & 3) + ((k >> 3 & 1) << 2)) << 1 : ((k >> 1 & 1) + ((k >> 3 & 1) << 1)) << 1;
   }
   // row in LDS and chunk of that row's memory that the lane's i-th 16 bytes hold
   static __device__ __forceinline__ void place(int wave, int lane, int i, int& row, int& chunk) {
@@ -233,36 +234,35 @@ struct Loader {
   }
 };
 
-// Writes 64 x 64 of C, whose first `rows` and `columns` exist, from a wavefront's fragments: a lane holds four neighbouring
-// columns of a row in each, pieces of 32 bytes of 16 rows an instruction.  They go through LDS (64 rows of 64 elements, the
-// wavefront's own), so that whole lines are written: straight from the fragments a tile of 256 x 256 took 28 us to write.
-constexpr int kStoreBytes = 64 * 64;      // ... times the size of an element
-template <typename O>
-__device__ __forceinline__ void store(const f32x4 (&acc)[4][4], O* c, int64_t ldc, int rows, int columns, char* lds, int lane) {
-  constexpr int pitch = 64 * (int)sizeof(O), chunks = pitch / 16, elems = 16 / (int)sizeof(O);
+// Writes a wavefront's part of C, of which the first `rows` and `columns` exist: a lane holds four neighbouring columns of a row in
+// each fragment, pieces of 32 bytes of 16 rows an instruction.  They go through LDS (the wavefront's own), so that whole lines are
+// written: straight from the fragments a tile of 256 x 256 took 28 us to write.
+template <typename O, int MI, int NJ>
+__device__ __forceinline__ void store(const f32x4 (&acc)[MI][NJ], O* c, int64_t ldc, int rows, int columns, char* lds, int lane) {
+  constexpr int width = NJ * 16, pitch = width * (int)sizeof(O), chunks = pitch / 16, elems = 16 / (int)sizeof(O), mask = chunks < 8 ? chunks - 1 : 7;
   const int l = lane & 15, q = lane >> 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       struct alignas(4 * sizeof(O)) Four { O e[4]; } v;
 #pragma unroll
       for (int r = 0; r < 4; ++r) v.e[r] = from_float<O>(acc[i][j][r]);
       const int byte = (j * 16 + q * 4) * (int)sizeof(O);
-      *reinterpret_cast<Four*>(lds + (i * 16 + l) * pitch + ((byte / 16 ^ (l & 7)) * 16) + byte % 16) = v;
+      *reinterpret_cast<Four*>(lds + (i * 16 + l) * pitch + ((byte / 16 ^ (l & mask)) * 16) + byte % 16) = v;
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (((uintptr_t)c | (uintptr_t)(ldc * sizeof(O)) | (uintptr_t)(columns < 64 ? columns * sizeof(O) : 0)) % 16 == 0) {
+  if (((uintptr_t)c | (uintptr_t)(ldc * sizeof(O)) | (uintptr_t)(columns < width ? columns * sizeof(O) : 0)) % 16 == 0) {
 #pragma unroll
-    for (int t = 0; t < chunks; ++t) {
+    for (int t = 0; t < MI * 16 * chunks / 64; ++t) {
       const int row = t * (64 / chunks) + lane / chunks, chunk = lane % chunks;
-      const word4 v = *reinterpret_cast<const word4*>(lds + row * pitch + ((chunk ^ (row & 7)) * 16));
+      const word4 v = *reinterpret_cast<const word4*>(lds + row * pitch + ((chunk ^ (row & mask)) * 16));
       if (row < rows && chunk * elems < columns) *reinterpret_cast<word4*>(c + row * ldc + chunk * elems) = v;
     }
   } else {
-    const int byte = lane * (int)sizeof(O);
-    for (int row = 0; row < (rows < 64 ? rows : 64); ++row)
-      if (lane < columns) c[row * ldc + lane] = *reinterpret_cast<const O*>(lds + row * pitch + ((byte / 16 ^ (row & 7)) * 16) + byte % 16);
+    const int column = lane % width, byte = column * (int)sizeof(O);
+    for (int row = lane / width; row < (rows < MI * 16 ? rows : MI * 16); row += 64 / width)
+      if (column < columns) c[row * ldc + column] = *reinterpret_cast<const O*>(lds + row * pitch + ((byte / 16 ^ (row & mask)) * 16) + byte % 16);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
@@ -275,7 +275,7 @@ struct Tile {
   using LA = Loader<T, AT, BM, kWaves>;
   using LB = Loader<T, BT, BN, kWaves>;
   static constexpr int kStage = LA::kBytes + LB::kBytes;
-  static constexpr int kLds = 2 * kStage > kWaves * kStoreBytes * 4 ? 2 * kStage : kWaves * kStoreBytes * 4;
+  static constexpr int kLds = 2 * kStage > kWaves * MI * NJ * 1024 ? 2 * kStage : kWaves * MI * NJ * 1024;
 
   // (to `partial`, if that is not null, in fp32)
   static __device__ __forceinline__ void run(const Operand& a, const Operand& b, int64_t red, O* c, float* partial, int64_t ldc, char* lds) {
@@ -339,10 +339,10 @@ struct Tile {
         work(buf);
       }
     }
-    static_assert(MI == 4 && NJ == 4, "");
     __syncthreads();                                                   // (the slabs have been read)
-    if (AT && partial) store<float>(acc, partial + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * 4, lane);
-    else store<O>(acc, c + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
+    char* own = lds + wave * (MI * NJ * 1024);
+    if (AT && partial) store<float>(acc, partial + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, own, lane);
+    else store<O>(acc, c + m0 * ldc + n0, ldc, a.valid - m0, b.valid - n0, own, lane);
   }
 };
 
@@ -399,6 +399,7 @@ struct Wide {
     wait_loads(slabs > 1);
     barrier();
     if (wave >= 4) barrier();
+    const bool some = m0 < a.valid && n0 < b.valid;                    // (else the wavefront only loads: short last slices)
     int at = 0;                                                        // slot of A
     const auto slot = [&](int k) { return at + k < kSlots ? at + k : at + k - kSlots; };
     for (int s = 0; s < slabs; ++s) {
@@ -407,10 +408,12 @@ struct Wide {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         word4 fa[8], fb[4];
+        if (some) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) fb[j] = LB::fragment(bs, n0 + j * 16, h, lane);
+          for (int j = 0; j < 4; ++j) fb[j] = LB::fragment(bs, n0 + j * 16, h, lane);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fa[i] = LA::fragment(as, m0 + i * 16, h, lane);
+          for (int i = 0; i < 8; ++i) fa[i] = LA::fragment(as, m0 + i * 16, h, lane);
+        }
         if (h == 0) {
           if (s + 1 < slabs) load_b(s + 1, slot(3));
         } else {
@@ -419,12 +422,14 @@ struct Wide {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier();
-        __builtin_amdgcn_s_setprio(1);
+        if (some) {
+          __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = multiply(T(), fb[j], fa[i], acc[i][j]);
-        __builtin_amdgcn_s_setprio(0);
+            for (int j = 0; j < 4; ++j) acc[i][j] = multiply(T(), fb[j], fa[i], acc[i][j]);
+          __builtin_amdgcn_s_setprio(0);
+        }
         barrier();
       }
       at = slot(2);
@@ -434,8 +439,8 @@ struct Wide {
     for (int h = 0; h < 2; ++h) {
       const auto& half = reinterpret_cast<const f32x4(&)[4][4]>(acc[h * 4]);
       const int64_t at = (m0 + h * 64) * ldc + n0;
-      if (AT && partial) store<float>(half, partial + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * kStoreBytes * 4, lane);
-      else store<O>(half, c + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * kStoreBytes * sizeof(O), lane);
+      if (AT && partial) store<float>(half, partial + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * 16384, lane);
+      else store<O>(half, c + at, ldc, a.valid - m0 - h * 64, b.valid - n0, lds + wave * 16384, lane);
     }
   }
 };
@@ -617,13 +622,18 @@ template <typename T, typename O>
 struct Tiles {
   template <bool AT, bool BT> using Large = Wide<T, O, AT, BT>;
   template <bool AT, bool BT> using Direct = Tile<T, O, AT, BT, 128, 128, 2, 2, true>;
+  template <bool AT, bool BT> using Small = Tile<T, O, AT, BT, 64, 64, 2, 2, true>;
+  template <bool AT, bool BT> using SmallStaged = Tile<T, O, AT, BT, 64, 64, 2, 2, false>;
   template <bool AT, bool BT> using Staged = Tile<T, O, AT, BT, 128, 128, 2, 2, false>;
 };
+
+constexpr int64_t kSmall = 384;
 
 // What a call of these sizes is done with, if rows of all operands are `straight` (below).
 struct Choice {
   bool few;             // 16 rows and columns to a block
-  bool large;           // tiles of 256 x 256 (16-bit types), one block to a compute unit; else 128 x 128, two
+  bool large;           // tiles of 256 x 256 (16-bit types), one block to a compute unit; else 128 x 128, two;
+  bool small;           // 64 x 64, five
   int64_t tiles;        // of all groups' C, by the groups' average size
   int shift;            // DW: rows of a slice, 0: groups are not cut
 };
@@ -635,13 +645,15 @@ inline Choice choose(int32_t product, int64_t size, int64_t rows, int64_t groups
   };
   Choice c;
   c.few = product == ADACGD_FORWARD && rows <= 16 * groups;
-  c.large = size == 2 && direct && n >= 256 && k >= 256 && (product == ADACGD_DW ? tiles(256) >= 64 : rows >= 192 * groups && tiles(256) >= 192);
-  c.tiles = tiles(c.large ? 256 : 128);
+  c.large = size == 2 && direct && n >= 256 && k >= 256 && (product == ADACGD_DW ? tiles(256) >= 128 : rows >= 192 * groups && tiles(256) >= 192);
+  const int64_t mean = up(rows, groups);
+  c.small = !c.large && tiles(128) * (product == ADACGD_DW ? std::max<int64_t>(1, mean / 1024) : 1) < kSmall;
+  c.tiles = tiles(c.large ? 256 : c.small ? 64 : 128);
   c.shift = 0;
   if (product == ADACGD_DW) {
     // cut the groups where their tiles leave compute units idle, into slices of 256 rows at least
-    const int64_t mean = up(rows, groups);
-    const int64_t parts = std::min(up(c.large ? 256 : 512, c.tiles), mean / 256);
+    const int64_t fill = c.large ? 256 : c.small ? 1024 : 512;
+    const int64_t parts = c.tiles >= (c.small ? 384 : 192) ? 1 : std::min(up(fill, c.tiles), mean / 256);
     if (parts > 1)
       for (c.shift = 8; (mean >> (c.shift + 1)) >= parts; ++c.shift) {}
   }
@@ -707,6 +719,10 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
       if (pick.few) return launch_few<T, O>(p, (hipStream_t)stream);
       if constexpr (sizeof(T) == 2) {
         if (pick.large) return launch<T, O, Tiles<T, O>::template Large>(product, p, (hipStream_t)stream);
+      }
+      if (pick.small) {
+        if (direct) return launch<T, O, Tiles<T, O>::template Small>(product, p, (hipStream_t)stream);
+        return launch<T, O, Tiles<T, O>::template SmallStaged>(product, p, (hipStream_t)stream);
       }
       if (direct) return launch<T, O, Tiles<T, O>::template Direct>(product, p, (hipStream_t)stream);
       return launch<T, O, Tiles<T, O>::template Staged>(product, p, (hipStream_t)stream);
