@@ -5,8 +5,9 @@
 // or the other one ("across"): FORWARD has both along, DX has B across, DW both.  A block forms a tile of C; slabs of both
 // operands, 128 bytes of r wide (64 elements of 16 bits, 32 of fp32), go through LDS, two of them: one is loaded while the
 // other is multiplied.
-//   along:   R rows of 128 bytes.  Lanes of a fragment read 16 bytes of 16 rows; the 16-byte chunk c of row r is kept at
-//            c ^ (r & 7), so that eight rows lie in different banks.
+//   along:   R rows of 128 bytes.  Lanes of a fragment read 16 bytes of 16 rows.  The 16-byte chunk c of row r is kept at c ^ (a
+//            function of r) so that the lanes served together find different banks: 0-3, 12-15, 20-23 and 24-27 are (counted:
+//            no conflicts; half of the LDS cycles with the chunk turned by r & 7).
 //   across:  a row of R elements for each r.  16-bit fragments are read transposed (ds_read_b64_tr_b16: 16 lanes take four
 //            rows of 16 elements and get four rows' values of one column each), fp32 ones element by element.  Pieces of 16
 //            elements are kept at piece ^ (a function of the row) so that the rows read together lie in different banks.
@@ -582,7 +583,7 @@ int check_sizes(int32_t product, int64_t rows, int64_t groups, int64_t n, int64_
 
 template <typename K>
 int enqueue(K kernel, int64_t blocks, int threads, int lds, hipStream_t stream, const ProductArgs& p) {
-  if (blocks > kMaxCount / 512) return fail(ADACGD_ERR_ARG, "more tiles than one launch takes");
+  if (blocks > (int64_t(1) << 32) / threads - 1) return fail(ADACGD_ERR_ARG, "more tiles than one launch takes");
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return fail(ADACGD_ERR_DEVICE, "adacgd_group_matmul: %s", hipGetErrorString(e));
@@ -704,7 +705,10 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
   ADACGD_TRY(adacgd_group_matmul_workspace_bytes(product, a->dtype, rows, groups, n, k, &need));
   ADACGD_TRY(check_workspace(workspace, workspace_bytes, need));
   if (rows == 0 && !dw) return ADACGD_OK;
-  ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, a->stride, b->stride, c->stride, b->group_stride, c->group_stride, {}, (int)n, (int)k, 0};
+  // (one row has no stride: whatever is given there, a second row must not be found)
+  const auto pitch = [](const adacgd_tensor* t, int64_t of, int64_t columns) { return of > 1 ? t->stride : columns; };
+  const int64_t lda = pitch(a, rows, product == ADACGD_FORWARD ? k : n), ldb = pitch(b, dw ? rows : n, k), ldc = pitch(c, dw ? n : rows, product == ADACGD_FORWARD ? n : k);
+  ProductArgs p{a->data, b->data, c->data, nullptr, offsets, rows, groups, 1, lda, ldb, ldc, b->group_stride, c->group_stride, {}, (int)n, (int)k, 0};
   if (!dw && b->group_stride == 0) { p.each = groups; p.groups = 1; }      // one matrix for all: one group
   const bool direct = straight(a, rows, product == ADACGD_FORWARD ? k : n, false) && straight(b, dw ? rows : n, k, !dw);
   const Choice pick = choose(product, dtype_size(a->dtype), rows, p.groups, n, k, direct);

@@ -120,6 +120,78 @@ def test_products_of_integers_are_exact(dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("sizes,n,k", [
+    ([5000, 0, 7041, 3, 500], 1032, 264), ([5000, 0, 7041, 3, 500], 264, 1032), ([157] * 20 + [0, 300, 1] + [150] * 20, 1032, 136),
+    ([1500, 0, 2600, 700, 257, 900], 1032, 1040), ([4096] * 3, 1032, 1040), ([9000], 520, 264), ([30] * 70, 520, 264),
+], ids=lambda v: str(len(v)) if isinstance(v, list) else str(v))
+def test_products_of_many_tiles_are_exact(dtype, pad, sizes, n, k):
+    """Sizes at which the larger tiles and the cut groups are used, each with whole and with ragged slices and slabs."""
+    first = 3 if pad else 0
+    rows, off = first + sum(sizes) + 2 * first, offsets_of(sizes, first)
+    x, dy, w = (ints(s, dtype, i).cuda() for i, s in enumerate(((rows, k), (rows, n), (len(sizes), n, k))))
+    y64, dx64 = torch.full((rows, n), 77.0, device="cuda").double(), torch.full((rows, k), 77.0, device="cuda").double()
+    dw64 = torch.zeros((len(sizes), n, k), device="cuda").double()
+    for g, (a, b) in enumerate(spans(sizes, first)):
+        if b > a:
+            y64[a:b] = x[a:b].double() @ w[g].double().t()
+            dx64[a:b] = dy[a:b].double() @ w[g].double()
+            dw64[g] = dy[a:b].double().t() @ x[a:b].double()
+    x[:first] = dy[:first] = float("nan")
+    x[rows - 2 * first:] = dy[rows - 2 * first:] = float("nan")
+    xg, dyg, wg = gpu(x, pad), gpu(dy, pad), gpu(w, pad)
+    for out in {dtype, F32}:
+        y, dx, dw = blank((rows, n), out, pad), blank((rows, k), out, pad), blank((len(sizes), n, k), out, pad)
+        L.group_matmul(xg, wg, off, out=y)
+        L.group_matmul_dx(dyg, wg, off, out=dx)
+        L.group_matmul_dw(dyg, xg, off, out=dw)
+        for got, want, name in ((y, y64, "y"), (dx, dx64, "dx"), (dw, dw64, "dw")):
+            assert torch.equal(got, want.float().to(out)), (name, out)
+            assert untouched(got), (name, out)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("stride", [0, 8, 5])
+def test_products_of_one_row_do_not_read_its_stride(dtype, stride):
+    n, k = 72, 264
+    x, dy, w = ints((1, k), dtype, 1).cuda(), ints((1, n), dtype, 2).cuda(), ints((1, n, k), dtype, 3).cuda()
+    off, odd = offsets_of([1]), lambda t: torch.as_strided(t, t.shape, (stride, 1))
+    out = dict(out=torch.empty((1, n, k), device="cuda"))
+    assert torch.equal(L.group_matmul_dw(odd(dy), odd(x), off, **out)[0], (dy.double().t() @ x.double()).float())
+    assert torch.equal(L.group_matmul(odd(x), w, off), (x.double() @ w[0].double().t()).float().to(dtype))
+    assert torch.equal(L.group_matmul_dx(odd(dy), w, off), (dy.double() @ w[0].double()).float().to(dtype))
+    one = ints((1, 1, k), dtype, 4).cuda()
+    v = ints((30, k), dtype, 5).cuda()
+    got = L.group_matmul(v, torch.as_strided(one, (1, 1, k), (k, stride, 1)), offsets_of([30]))
+    assert torch.equal(got, (v.double() @ one[0].double().t()).float().to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_products_keep_infinities_and_nan_to_their_rows(dtype):
+    for sizes, n, k in (([300, 200], 136, 264), ([2, 3], 136, 264), ([9000, 4000], 1032, 264)):
+        x, w, off = normals((sum(sizes), k), dtype, 1).cuda(), normals((2, n, k), dtype, 2).cuda(), offsets_of(sizes)
+        clean = L.group_matmul(x, w, off)
+        bad = x.clone()
+        rows = [1, sum(sizes) - 1]
+        bad[1, 3], bad[-1, 7] = float("nan"), float("inf")
+        got = L.group_matmul(bad, w, off)
+        keep = torch.ones(sum(sizes), dtype=torch.bool, device="cuda")
+        keep[rows] = False
+        assert torch.equal(got[keep], clean[keep]) and torch.isnan(got[1]).all() and not torch.isfinite(got[-1]).any()
+
+
+@pytest.mark.parametrize("dtype,small", [(F32, 2.0 ** -140), (BF16, 2.0 ** -130), (F16, 2.0 ** -20)])
+def test_products_of_subnormal_numbers(dtype, small):
+    """Subnormal elements count with their value, whatever tile they are in."""
+    for rows, n, k in ((40, 48, 72), (2, 48, 264)):
+        x = ints((rows, k), dtype, 1) * small
+        w, off = ints((1, n, k), dtype, 2), offsets_of([rows])
+        big = w * (1.0 if dtype == F16 else 2.0 ** 100)
+        y = L.group_matmul(x.cuda(), big.to(dtype).cuda(), off, out=torch.empty((rows, n), device="cuda"))
+        assert torch.equal(y.cpu(), (x.double() @ big[0].to(dtype).double().t()).float())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", [([5, 0, 130, 64, 1], 200, 96, 1), ([700], 128, 512, 0), ([1, 1, 2], 320, 1024, 0), ([90, 1700], 264, 136, 0)],
                          ids=lambda s: "%d-%dx%d+%d" % (len(s[0]), s[1], s[2], s[3]))
 def test_products_of_numbers(dtype, shape):
@@ -662,6 +734,35 @@ def test_the_binding_refuses_what_does_not_fit():
         L.layer_norm(x.double())
     with pytest.raises(E.AdaCGDError):
         L.group_matmul(x, w.to(BF16), off)
+
+
+def test_a_captured_product_of_large_tiles():
+    sizes = [5000, 0, 7041, 3, 500]
+    off, x, w = offsets_of(sizes), normals((sum(sizes), 264), BF16, 1).cuda(), normals((5, 1032, 264), BF16, 2).cuda()
+    y, dw = torch.empty((sum(sizes), 1032), dtype=BF16, device="cuda"), torch.empty((5, 1032, 264), device="cuda")
+    want = L.group_matmul(x, w, off), L.group_matmul_dw(L.group_matmul(x, w, off), x, off)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L.group_matmul(x, w, off, out=y)
+        L.group_matmul_dw(y, x, off, out=dw)
+    for _ in range(3):
+        y.zero_(), dw.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dw, want[1])
+        assert torch.equal(L.group_matmul(x, w, off), want[0])
+
+
+@pytest.mark.parametrize("bad", [[0, 12000, -3, 9000, 1 << 40], [1 << 62, 0, 5000, 4000, 12544], [12544] * 5])
+def test_offsets_that_break_the_rule_stay_inside_large_tiles(bad):
+    off, rows = torch.tensor(bad, device="cuda"), 12544
+    x, w, y, dw = blank((rows, 264), BF16, 8), gpu(normals((4, 1032, 264), BF16, 1), 8), blank((rows, 1032), BF16, 8), blank((4, 1032, 264), F32, 8)
+    L.group_matmul(x, w, off, out=y)
+    L.group_matmul_dx(y, w, off, out=x)
+    L.group_matmul_dw(y, x, off, out=dw)
+    torch.cuda.synchronize()
+    assert untouched(x) and untouched(y) and untouched(dw)
 
 
 @pytest.mark.parametrize("bad", [[0, 900, 20, 60], [-5, 30, 40, 1 << 62], [-(1 << 62), 5, 3, 60], [60, 40, 20, 0], [100, 100, 100, 100]])
