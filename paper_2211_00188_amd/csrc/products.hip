@@ -181,7 +181,32 @@ struct Loader {
       }
     }
   }
-  // Through registers: any alignment and any pitch.
+  // Through registers: any alignment and any pitch.  Of slabs that rows follow (across) or that end inside the rows (along), whole
+  // chunks are read whatever they hold past the tile's rows and columns, which only elements of C that are not written depend on:
+  // rows that do not exist are read as the last one, chunks that begin past the columns as the first, and one that passes the columns
+  // ends in the next row (of 16 bytes at least).
+  const char* at[kLoads];
+  int64_t step;
+  __device__ __forceinline__ void begin(const Operand& o, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row, chunk;
+      place(wave, lane, i, row, chunk);
+      const int q = ACROSS ? (chunk * kElem < o.valid ? chunk * kElem : 0) : (row < o.valid ? row : o.valid - 1);
+      at[i] = o.p + (ACROSS ? (int64_t)row * o.pitch + q * (int)sizeof(T) : (int64_t)q * o.pitch + chunk * 16);
+    }
+    step = ACROSS ? kDepth * o.pitch : kSlab;
+  }
+  __device__ __forceinline__ void next(const Operand& o, int64_t red, int64_t r0, word4 (&st)[kLoads], int wave, int lane) {
+    if (ACROSS ? r0 + kDepth < red && o.pitch >= 16 : r0 + kDepth <= red) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) __builtin_memcpy(&st[i], at[i], 16);
+    } else {
+      fetch(o, red, r0, st, wave, lane);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) at[i] += step;
+  }
   __device__ __forceinline__ void fetch(const Operand& o, int64_t red, int64_t r0, word4 (&st)[kLoads], int wave, int lane) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -325,8 +350,10 @@ struct Tile {
     } else {
       word4 sa[LA::kLoads], sb[LB::kLoads];
       if (slabs > 0) {
-        la.fetch(a, red, 0, sa, wave, lane);
-        lb.fetch(b, red, 0, sb, wave, lane);
+        la.begin(a, wave, lane);
+        lb.begin(b, wave, lane);
+        la.next(a, red, 0, sa, wave, lane);
+        lb.next(b, red, 0, sb, wave, lane);
       }
       for (int64_t s = 0; s < slabs; ++s) {
         char* buf = lds + (s & 1) * kStage;
@@ -334,8 +361,8 @@ struct Tile {
         LB::put(sb, buf + LA::kBytes, wave, lane);
         __syncthreads();
         if (s + 1 < slabs) {
-          la.fetch(a, red, (s + 1) * LA::kDepth, sa, wave, lane);
-          lb.fetch(b, red, (s + 1) * LA::kDepth, sb, wave, lane);
+          la.next(a, red, (s + 1) * LA::kDepth, sa, wave, lane);
+          lb.next(b, red, (s + 1) * LA::kDepth, sb, wave, lane);
         }
         work(buf);
       }
