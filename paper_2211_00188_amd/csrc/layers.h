@@ -102,6 +102,21 @@ __device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t grou
   return s;
 }
 
+// The last group that begins at or before `row` (0 if none does), 64 of them looked at with one load.  For all lanes of a wavefront.
+__device__ __forceinline__ int64_t group_of(const int64_t* offsets, int64_t groups, int64_t rows, int64_t row) {
+  const int lane = (int)lane_id();
+  int64_t low = 0, count = groups;
+  while (count > 1) {
+    const int64_t step = (count + 63) / 64;
+    const bool here = lane * step < count;
+    const uint64_t m = ballot(here && offset_at(offsets, low + (here ? lane * step : 0), rows) <= row);
+    const int64_t hit = m ? 63 - __builtin_clzll(m) : 0;
+    low += hit * step;
+    count = count - hit * step < step ? count - hit * step : step;
+  }
+  return low;
+}
+
 // First number of a group's slices.
 __device__ __forceinline__ int64_t first_number(int64_t first_row, int64_t group, int shift) { return (first_row >> shift) + group; }
 

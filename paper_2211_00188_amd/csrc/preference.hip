@@ -140,7 +140,7 @@ template <typename T, int TPR>
 __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequences, int64_t v, const float* dloss, const T* logits, int64_t ld, const int64_t* targets,
                                                     const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, Parts parts, T* out, int64_t ldo) {
   constexpr int E = Vec<T>::kElems, PER = 256 / TPR;
-  const int t0 = threadIdx.x % TPR, lane = (int)lane_id();
+  const int t0 = threadIdx.x % TPR;
   const int64_t first = offset_at(offsets, 0, tokens), last = offset_at(offsets, sequences, tokens);
   for (int64_t u = (int64_t)blockIdx.x * PER + threadIdx.x / TPR; u < tokens * parts.count; u += (int64_t)gridDim.x * PER) {
     const int64_t t = u / parts.count, begin = (u - t * parts.count) * parts.length;
@@ -154,16 +154,7 @@ __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequ
       for (int64_t c = begin + t0 * E; c < end; c += TPR * E) zero.store(o + c, end - c);
       continue;
     }
-    // the last sequence that begins at or before t: 64 of them looked at with one load
-    int64_t low = 0, count = sequences;
-    while (count > 1) {
-      const int64_t step = (count + 63) / 64;
-      const bool here = lane * step < count;
-      const uint64_t m = ballot(here && offset_at(offsets, low + (here ? lane * step : 0), tokens) <= t);
-      const int64_t hit = m ? 63 - __builtin_clzll(m) : 0;
-      low += hit * step;
-      count = count - hit * step < step ? count - hit * step : step;
-    }
+    const int64_t low = group_of(offsets, sequences, tokens, t);
     const double z = beta * (double)margin[low / 2];
     const double slope = (smoothing / (1 + exp(-z)) - (1 - smoothing) / (1 + exp(z))) * beta * (double)dloss[low / 2];
     const float f = (float)(low % 2 ? -slope : slope), l = lse[t];

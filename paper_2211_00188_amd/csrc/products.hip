@@ -52,7 +52,8 @@ inline int64_t patch_blocks(const Patches& p) {
 }
 __device__ __forceinline__ bool tile_of(uint32_t block, const Patches& p, int64_t& i, int64_t& j) {
   const uint32_t columns = (uint32_t)patch_columns(p);
-  const uint32_t patch = (block >> (3 + p.lp)) * 8 + (block & 7), in = block >> 3 & ((1u << p.lp) - 1);
+  // (eight patches in turn begin at another die each time: what returns every few patches, such as numbers without a slice, is not one die's)
+  const uint32_t turn = block >> (3 + p.lp), patch = turn * 8 + ((block + 3 * turn) & 7), in = block >> 3 & ((1u << p.lp) - 1);
   const uint32_t row = patch / columns;
   i = ((int64_t)row << (p.lp - p.lw)) + (in >> p.lw);
   j = ((int64_t)(patch - row * columns) << p.lw) + (in & ((1u << p.lw) - 1));
@@ -67,13 +68,18 @@ struct ProductArgs {
   const void* a;
   const void* b;
   void* c;
-  float* partial;                       // DW: sums of slices [numbers][n][k], where groups are cut; else null
+  float* partial;                       // DW: sums of slices [part_number][n][k], where groups are cut; else null
   const int64_t* offsets;
   int64_t rows, groups, each;           // `each` entries of offsets to a group
   int64_t lda, ldb, ldc, gsb, gsc;
   Patches patches;
   int n, k, shift;
 };
+
+// Where the sums of a cut group's slices lie: from 2 (first row >> shift) on.  Only groups of more than 2^shift rows are cut, so that the
+// next of them begins behind the last slice, and the number of places does not depend on the number of groups.
+__host__ __device__ inline int64_t part_number(int64_t first, int shift) { return 2 * (first >> shift); }
+inline int64_t part_numbers(int64_t rows, int shift) { return 2 * (rows >> shift) + 1; }
 
 // The block's tile among those of slices that exist, of at most 64 groups.
 __device__ __forceinline__ bool find_tile(const ProductArgs& p, Slice& s, int64_t& j) {
@@ -502,34 +508,43 @@ __global__ void __launch_bounds__(K::kThreads) k_group_product(ProductArgs p) {
   int64_t i, j;
   if (!tile_of(blockIdx.x, p.patches, i, j)) return;
   const int64_t number = i / tn, n0 = (i - number * tn) * BM, k0 = j * BN;
+  // The first numbers are the groups, with their first slice; further slices belong to the multiples of a slice's rows that lie behind
+  // a group's first row, the i-th of them to slice i.  So only these are searched for.
   Slice s;
-  if (p.partial) {
-    s = find_slice(p.offsets, p.groups, p.rows, 1, p.shift, number);
-    if (s.group < 0) return;
-  } else {                                       // one slice to a group
-    s.group = number;
-    s.begin = s.first = offset_at(p.offsets, number, p.rows);
-    s.end = s.last = offset_at(p.offsets, number + 1, p.rows);
-    if (s.end < s.begin) s.end = s.last = s.begin;
+  const int64_t row = (number - p.groups + 1) << p.shift;
+  s.group = number < p.groups ? number : group_of(p.offsets, p.groups, p.rows, row);
+  s.first = offset_at(p.offsets, s.group, p.rows);
+  s.last = offset_at(p.offsets, s.group + 1, p.rows);
+  if (s.last < s.first) s.last = s.first;
+  s.begin = s.first;
+  if (number >= p.groups) {
+    if (row <= s.first || row >= s.last) return;
+    s.begin += (row >> p.shift) - (s.first >> p.shift) << p.shift;
+    if (s.begin >= s.last) return;
   }
+  s.end = p.partial && s.begin + (int64_t(1) << p.shift) < s.last ? s.begin + (int64_t(1) << p.shift) : s.last;
   const Operand a{(const char*)p.a + (s.begin * p.lda + n0) * (int)sizeof(T), p.lda * (int)sizeof(T), (int)(p.n - n0)};
   const Operand b{(const char*)p.b + (s.begin * p.ldb + k0) * (int)sizeof(T), p.ldb * (int)sizeof(T), (int)(p.k - k0)};
   if (p.partial && s.last - s.first > int64_t(1) << p.shift)
-    K::run(a, b, s.end - s.begin, nullptr, p.partial + (number * p.n + n0) * p.k + k0, p.k, lds);
+    K::run(a, b, s.end - s.begin, nullptr,
+           p.partial + ((part_number(s.first, p.shift) + ((s.begin - s.first) >> p.shift)) * p.n + n0) * p.k + k0, p.k, lds);
   else
     K::run(a, b, s.end - s.begin, (O*)p.c + s.group * p.gsc + n0 * p.ldc + k0, nullptr, p.ldc, lds);
 }
 
-// Sums of the slices of every group that has several, in their order.
+// Sums of the slices of every group that has several, in their order.  A group that is cut holds a multiple of a slice's rows; it is
+// done by the blocks of the first of these, so that there are as many as slices and not as groups (a thousand groups of which none
+// is cut: 25 us).
 template <typename O>
 __global__ void __launch_bounds__(256) k_join(ProductArgs p) {
-  const int64_t g = blockIdx.y;
+  const int64_t row = (int64_t)blockIdx.y << p.shift;
+  const int64_t g = group_of(p.offsets, p.groups, p.rows, row);
   const int64_t first = offset_at(p.offsets, g, p.rows), last = offset_at(p.offsets, g + 1, p.rows);
   const int64_t count = (last - first + (int64_t(1) << p.shift) - 1) >> p.shift;
-  if (count <= 1) return;
+  if (last <= row || first > row || count <= 1 || row - first >= int64_t(1) << p.shift) return;
   const int64_t size = (int64_t)p.n * p.k, e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (e >= size) return;
-  const float* from = p.partial + first_number(first, g, p.shift) * size + e;
+  const float* from = p.partial + part_number(first, p.shift) * size + e;
   const int64_t have = size - e;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -625,10 +640,11 @@ int launch(int32_t product, ProductArgs p, hipStream_t stream) {
   constexpr int BM = K<true, true>::kRows, BN = K<true, true>::kColumns, threads = K<true, true>::kThreads, lds = K<true, true>::kLds;
   if (product == ADACGD_DW) {
     const int64_t tn = (p.n + BM - 1) / BM, tk = (p.k + BN - 1) / BN;
-    p.patches = patches_of((p.partial ? slice_numbers(p.rows, p.groups, p.shift) : p.groups) * tn, tk, tn * tk);
+    p.patches = patches_of((p.groups + (p.partial ? p.rows >> p.shift : 0)) * tn, tk, tn * tk);
     ADACGD_TRY((enqueue(k_group_product<T, O, K<true, true>>, patch_blocks(p.patches), threads, lds, stream, p)));
     if (!p.partial) return ADACGD_OK;
-    k_join<O><<<dim3(((int64_t)p.n * p.k + 1023) / 1024, p.groups), 256, 0, stream>>>(p);
+    // (rows >> shift is below twice the parts of all groups, some 2800, or a quarter of the groups: see choose)
+    k_join<O><<<dim3(((int64_t)p.n * p.k + 1023) / 1024, (p.rows >> p.shift) + 1), 256, 0, stream>>>(p);
     return launched("adacgd_group_matmul");
   }
   p.shift = __builtin_ctz(BM);
@@ -682,8 +698,13 @@ inline Choice choose(int32_t product, int64_t size, int64_t rows, int64_t groups
     // cut the groups where their tiles leave compute units idle, into slices of 256 rows at least
     const int64_t fill = c.large ? 256 : c.small ? 1024 : 512;
     const int64_t parts = c.tiles >= (c.small ? 384 : 192) ? 1 : std::min(up(fill, c.tiles), mean / 256);
-    if (parts > 1)
+    if (parts > 1) {
       for (c.shift = 8; (mean >> (c.shift + 1)) >= parts; ++c.shift) {}
+    } else if (groups > 1 && c.tiles <= 32 * groups) {
+      // groups of few tiles: one much longer than the others would keep as few compute units for its whole length
+      for (c.shift = 11; (int64_t(1) << c.shift) < 4 * mean; ++c.shift) {}
+      if (rows <= int64_t(1) << c.shift) c.shift = 0;
+    }
   }
   return c;
 }
@@ -711,7 +732,7 @@ int adacgd_group_matmul_workspace_bytes(int32_t product, int32_t dtype, int64_t 
     // (for either alignment of the operands: the tensors are not known here)
     for (const bool direct : {false, true}) {
       const int shift = choose(product, dtype_size(dtype), rows, groups, n, k, direct).shift;
-      if (shift) *bytes = std::max(*bytes, (slice_numbers(rows, groups, shift) * n * k * 4 + 255) / 256 * 256);
+      if (shift) *bytes = std::max(*bytes, (part_numbers(rows, shift) * n * k * 4 + 255) / 256 * 256);
     }
   }
   return ADACGD_OK;

@@ -124,6 +124,7 @@ def test_products_of_integers_are_exact(dtype, shape):
 @pytest.mark.parametrize("sizes,n,k", [
     ([5000, 0, 7041, 3, 500], 1032, 264), ([5000, 0, 7041, 3, 500], 264, 1032), ([157] * 20 + [0, 300, 1] + [150] * 20, 1032, 136),
     ([1500, 0, 2600, 700, 257, 900], 1032, 1040), ([4096] * 3, 1032, 1040), ([9000], 520, 264), ([30] * 70, 520, 264),
+    ([1] * 100 + [0, 9001] + [3] * 400, 264, 136), ([2049, 2048, 5000, 0] + [2] * 300, 72, 136),
 ], ids=lambda v: str(len(v)) if isinstance(v, list) else str(v))
 def test_products_of_many_tiles_are_exact(dtype, pad, sizes, n, k):
     """Sizes at which the larger tiles and the cut groups are used, each with whole and with ragged slices and slabs."""

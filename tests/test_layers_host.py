@@ -140,3 +140,17 @@ def test_numbers_of_slices_ascend_without_a_prefix_sum(shift):
         rows = int(o[-1] + rng.integers(0, 2 << shift))
         numbers = [(int(o[g]) >> shift) + g + j for g in range(groups) for j in range(max(1, -(-int(sizes[g]) >> shift)))]
         assert all(a < b for a, b in zip(numbers, numbers[1:])) and numbers[-1] < (rows >> shift) + groups
+
+
+@pytest.mark.parametrize("shift", [8, 9, 11, 13])
+def test_places_of_cut_groups_sums_do_not_meet(shift):
+    """2 (first row >> shift) + j for the slices of groups of more than 2^shift rows: no two alike, all below 2 (rows >> shift) + 1."""
+    rng = np.random.default_rng(shift)
+    for trial in range(300):
+        groups = int(rng.integers(1, 30))
+        sizes = (rng.integers(0, 4 << shift, groups) * (rng.random(groups) < 0.7)).astype(int)
+        sizes[rng.random(groups) < 0.3] = (1 << shift) + int(rng.integers(-1, 2))
+        o = int(rng.integers(0, 2 << shift)) + np.concatenate([[0], np.cumsum(sizes)])
+        rows = int(o[-1])
+        places = [2 * (int(o[g]) >> shift) + j for g in range(groups) if sizes[g] > 1 << shift for j in range(-(-int(sizes[g]) >> shift))]
+        assert len(set(places)) == len(places) and max(places, default=0) < 2 * (rows >> shift) + 1
