@@ -688,16 +688,27 @@ inline Choice choose(int32_t product, int64_t size, int64_t rows, int64_t groups
     return groups * up(up(rows, groups), t) * up(product == ADACGD_FORWARD ? n : k, t);
   };
   Choice c;
-  c.few = product == ADACGD_FORWARD && rows <= 16 * groups;
+  // 16 rows and columns to a block: one group's weights of 4096 x 4096 take 8 us with one row and 17 with 16, in tiles of 64, which are
+  // too few then, 32 and 34; eight groups' take 41 us with a row each (tiles 49), but 61 and 75 with 8 and 16 each (tiles 53 and 53),
+  // because the rows are read again for every 16 columns
+  c.few = product == ADACGD_FORWARD && (rows <= 4 * groups || (rows <= 16 * groups && groups * up(n, 64) < 256));
+  // 256 x 256, a block to a compute unit, when they fill three quarters of the card: 8192 rows, 2048 x 2048 by rows 67 us (tiles of 128: 74),
+  // 16384 rows, 4096 x 2048 211 (320); with half as many tiles 55 (35 and 45: 4096 rows, 2048 x 2048).  Groups of under 192 rows
+  // leave more than a quarter of a tile empty.  The groups' sums can be cut, which costs what their partial sums do
   c.large = size == 2 && direct && n >= 256 && k >= 256 && (product == ADACGD_DW ? tiles(256) >= 128 : rows >= 192 * groups && tiles(256) >= 192);
   const int64_t mean = up(rows, groups);
+  // 64 x 64, five to a compute unit, when tiles of 128 (two to one) are fewer than three quarters of their places: 2030 fp32 rows in ten
+  // groups, 503 x 1001 46 us (tiles of 128: 84), 2048 bf16 rows, 1024 x 1024 10 (14); with enough tiles 4096 rows, 2048 x 1024 30 (22)
   c.small = !c.large && tiles(128) * (product == ADACGD_DW ? std::max<int64_t>(1, mean / 1024) : 1) < kSmall;
   c.tiles = tiles(c.large ? 256 : c.small ? 64 : 128);
   c.shift = 0;
   if (product == ADACGD_DW) {
-    // cut the groups where their tiles leave compute units idle, into slices of 256 rows at least
+    // cut the groups where their tiles leave compute units idle, into slices of 256 rows at least: 65536 rows, 512 x 512 bf16 51 us
+    // (whole: 1200), 16384 rows, 4096 x 2048 in tiles of 256 235 (390).  Half of the places of tiles of 128 are enough for
+    // short groups (2048 rows, 2048 x 2048: 38 whole, 45 cut; 8192 rows: 139 whole, 87 cut)
     const int64_t fill = c.large ? 256 : c.small ? 1024 : 512;
-    const int64_t parts = c.tiles >= (c.small ? 384 : 192) ? 1 : std::min(up(fill, c.tiles), mean / 256);
+    const int64_t enough = c.small || (!c.large && mean >= 4096) ? 384 : 192;
+    const int64_t parts = c.tiles >= enough ? 1 : std::min(up(fill, c.tiles), mean / 256);
     if (parts > 1) {
       for (c.shift = 8; (mean >> (c.shift + 1)) >= parts; ++c.shift) {}
     } else if (groups > 1 && c.tiles <= 32 * groups) {
