@@ -690,8 +690,10 @@ inline Choice choose(int32_t product, int64_t size, int64_t rows, int64_t groups
   Choice c;
   // 16 rows and columns to a block: one group's weights of 4096 x 4096 take 8 us with one row and 17 with 16, in tiles of 64, which are
   // too few then, 32 and 34; eight groups' take 41 us with a row each (tiles 49), but 61 and 75 with 8 and 16 each (tiles 53 and 53),
-  // because the rows are read again for every 16 columns
-  c.few = product == ADACGD_FORWARD && (rows <= 4 * groups || (rows <= 16 * groups && groups * up(n, 64) < 256));
+  // because the rows are read again for every 16 columns.  Tiles of 64 columns that leave half of the card idle lose up to 64 rows:
+  // 64 rows, 1024 x 1024 5 us (8), 256 x 4096 10 (22), 4 x 16 rows, 2048 x 2048 17 (19)
+  const int64_t wide = groups * up(n, 64);
+  c.few = product == ADACGD_FORWARD && (rows <= 4 * groups || (wide < 256 && rows <= (wide <= 128 ? 64 : 16) * groups));
   // 256 x 256, a block to a compute unit, when they fill three quarters of the card: 8192 rows, 2048 x 2048 by rows 67 us (tiles of 128: 74),
   // 16384 rows, 4096 x 2048 211 (320); with half as many tiles 55 (35 and 45: 4096 rows, 2048 x 2048).  Groups of under 192 rows
   // leave more than a quarter of a tile empty.  The groups' sums can be cut, which costs what their partial sums do
