@@ -350,15 +350,16 @@ const char* adacgd_last_error(const adacgd_ctx* ctx);
  *    only; rows that begin on 16 bytes are read and written faster.
  *  - offsets is a DEVICE array of groups + 1 row numbers: group g owns rows [offsets[g], offsets[g+1]).  They must
  *    ascend and lie in [0, rows]; equal ones leave a group empty.  The host does not read them.  Offsets that break
- *    the rule give unspecified results, but nothing outside the matrices is read or written.  Rows before the first
- *    and behind the last group are neither read nor written in any output that has a row for each of them.
- *  - Sums are held in fp32 or fp64 and are formed in an order that depends on the sizes only: the same call gives the
- *    same bits.
+ *    the rule give unspecified results, but nothing outside the matrices is read or written.  What inputs hold in
+ *    rows before the first and behind the last group does not matter, and outputs keep what they hold there.
+ *  - Sums are held in fp32 or fp64 and are formed in an order that depends on sizes, offsets, strides and alignment
+ *    only: the same call gives the same bits.
  *  - Everything is enqueued on `stream` (a hipStream_t of the current device); no call allocates, synchronises or
  *    keeps anything.  All of them may be captured into a graph.  A workspace is needed until the enqueued work has
  *    completed and must not be shared by calls that may run at the same time; it need not be cleared.
  *  - Outputs must not overlap inputs or each other, except where stated.
- *  - Limits: rows below 2^31, at most 65535 groups or 2^22 pairs, rows of at most 2^24 elements, strides below 2^31. */
+ *  - Limits: rows below 2^31, at most 65535 groups or 2^22 pairs, rows of at most 2^24 elements, strides below
+ *    2^31, and what one launch takes (2^32 threads: some 16 million tiles of 128 x 128; ADACGD_ERR_ARG beyond). */
 enum adacgd_dtype { ADACGD_FP32 = 0, ADACGD_BF16 = 1, ADACGD_FP16 = 2 };
 
 typedef struct {
