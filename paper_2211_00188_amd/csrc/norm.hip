@@ -10,8 +10,11 @@ namespace {
 
 // A row is held in registers: `TPR` threads, `NV` vectors of 16 bytes each, vector i of thread t being number i TPR + t of the
 // row, so that x is read once whatever is made of it.  One wavefront to a row needs no barrier; rows past what 1024 threads
-// hold are read again (they are in cache).  The least threads that hold the row are taken.  Bound by memory: a pass over
-// x and one over y, or over dy, x and dx.
+// hold are read again (they are in cache).  The least threads that hold the row are taken, with one or two vectors each: four need
+// the registers that rows on their way ahead take (65536 x 2048 bf16: 168 us by a wavefront to a row, 119 by 256 threads), and rows
+// of 64 and 256 elements by 16 lanes take 71 and 65 us where a wavefront to each takes 71 to 88 (10^6 and 3 10^5 rows, forward) and
+// 130 and 110 where it takes 203 and 215 (backward).  Bound by memory: a pass over x and one over y, or over dy, x and dx; 65536 x 2048
+// bf16 119 us forward (4.5 TB/s) and 199 backward (4.0), fp32 213 and 330 (5.0 and 4.9).
 template <int TPR, int BLOCK>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
   if constexpr (TPR == 16) return row16_sumf(v);
@@ -284,7 +287,8 @@ __global__ void __launch_bounds__(256) k_norm_long_sums(const int64_t* offsets, 
   if (ob) ob[c] = sb;
 }
 
-// Sums of the slices of every group that has several.  32 columns by 32 threads that share the slices.
+// Sums of the slices of every group that has several.  32 columns by 32 threads that share the slices (1024 slices of 2048 columns:
+// 11 us; one thread to a column would wait for each in turn).
 __global__ void __launch_bounds__(1024) k_norm_join(const int64_t* offsets, int64_t rows, int d, Columns out) {
   __shared__ double part[32][33];
   const int64_t g = blockIdx.y;
@@ -341,7 +345,8 @@ bool by_width(int64_t d, F f) {
 
 // One block of Philox gives the draws of eight neighbouring elements (16 bits each); a thread does those eight.  They begin at
 // multiples of eight of the element's number, wherever these lie in memory.  Rows that follow each other without gaps are one row.
-// Bound by memory; the generator's 20 wide products for eight elements take half of the time that a pass over 16-bit x and out does.
+// Bound by memory: 65536 x 2048 bf16 with a residual 149 us (5.4 TB/s), without one 96; a copy reaches 5.1.  One element a thread, and
+// a generator block for each, took 500.
 template <typename T>
 __global__ void __launch_bounds__(256) k_dropout(const T* x, int64_t ldx, const T* residual, int64_t ldr, T* out, int64_t ldo, int64_t rows, int64_t d,
                                                  uint32_t cut, float scale, uint64_t seed, uint32_t step, const int64_t* step_dev, uint32_t layer,

