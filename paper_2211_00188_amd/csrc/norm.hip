@@ -11,10 +11,10 @@ namespace {
 // A row is held in registers: `TPR` threads, `NV` vectors of 16 bytes each, vector i of thread t being number i TPR + t of the
 // row, so that x is read once whatever is made of it.  One wavefront to a row needs no barrier; rows past what 1024 threads
 // hold are read again (they are in cache).  The least threads that hold the row are taken, with one or two vectors each: four need
-// the registers that rows on their way ahead take (65536 x 2048 bf16: 168 us by a wavefront to a row, 119 by 256 threads), and rows
-// of 64 and 256 elements by 16 lanes take 71 and 65 us where a wavefront to each takes 71 to 88 (10^6 and 3 10^5 rows, forward) and
-// 130 and 110 where it takes 203 and 215 (backward).  Bound by memory: a pass over x and one over y, or over dy, x and dx; 65536 x 2048
-// bf16 119 us forward (4.5 TB/s) and 199 backward (4.0), fp32 213 and 330 (5.0 and 4.9).
+// the registers that rows on their way ahead take (65536 x 2048 bf16 forward: 168 us by a wavefront to a row, 119 by 256 threads).  Short
+// rows share a wavefront: 10^6 of 64 elements 71 us forward (289 by a wavefront each), 3 10^5 of 256 elements 65 us forward and 110
+// backward (87 and 215).  Bound by memory: a pass over x and one over y, or over dy, x and dx; 65536 x 2048 bf16 119 us forward
+// (4.5 TB/s) and 199 backward (4.0), fp32 213 and 330 (5.0 and 4.9).
 template <int TPR, int BLOCK>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
   if constexpr (TPR == 16) return row16_sumf(v);
