@@ -426,7 +426,9 @@ int adacgd_preference_loss(int64_t tokens, int64_t pairs, int64_t v, const adacg
                            float* margin, float* logp, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* dlogits = sum_p dloss[p] d loss[p] / d logits, zero at tokens that do not count; dloss: fp32 [pairs].  dlogits has the
- * type of logits and may be logits. */
+ * type of logits and may be logits.  The slope of the loss is that at margin as it is given, in fp32: a relative error of up to
+ * 2^-24 |beta margin|.  What rounding lse to fp32 took from it does not enter: where that could be seen in dlogits' type, the rows'
+ * sums are formed again around lse. */
 int adacgd_preference_loss_backward(int64_t tokens, int64_t pairs, int64_t v, const float* dloss, const adacgd_tensor* logits,
                                     const int64_t* targets, const int64_t* offsets, const float* margin, const float* lse,
                                     double beta, double smoothing, const adacgd_tensor* dlogits, void* stream);

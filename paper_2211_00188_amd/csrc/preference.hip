@@ -30,9 +30,12 @@ struct Parts {
   int64_t count, length;
 };
 constexpr int kUnroll = 4;      // vectors of a thread on their way
-inline Parts parts_of(int64_t tokens, int64_t v) {
+constexpr int64_t kTokenBlocks = 1024;
+// Where every part of a row reads all of it for its sum (k_token_grad): 61 rows of 128000 fp32 30 us (44 by 1024 blocks), 250 58 (113).
+constexpr int64_t kSumBlocks = 256;
+inline Parts parts_of(int64_t tokens, int64_t v, int64_t blocks = kTokenBlocks) {
   const int64_t unit = 2048;
-  int64_t count = tokens > 0 ? 1024 / tokens : 1;
+  int64_t count = tokens > 0 ? blocks / tokens : 1;
   const int64_t most = (v + unit - 1) / unit;
   count = count < 1 ? 1 : count > most ? most : count;
   const int64_t length = ((v + count - 1) / count + unit - 1) / unit * unit;
@@ -137,18 +140,25 @@ __global__ void __launch_bounds__(kPairThreads) k_pair(int64_t tokens, int64_t v
   }
 }
 
-// dlogits of (a part of) every row: f (onehot - exp(x - lse)), f from the margin of the row's pair.  Bound by memory: 8192 x 32000
-// bf16 202 us (5.2 TB/s).
+// dlogits of (a part of) every row: f (onehot - p), f from the margin of the row's pair, p = exp(x - lse).  lse was rounded to fp32, by
+// up to 2^-24 of its own size, which is a relative error of every p of the row (and all of p where the elements are the type's
+// lowest: lse has lost the logarithm of their number).  While that is at most 1/64 of what storing the result loses, |lse| <= 1024 in
+// bf16 and 128 in fp16, it stays.  Otherwise, in fp32 nearly always, the row's sum is formed anew around lse, where x - lse has no
+// such error, and divided by; the row is read twice then.  Bound by memory: 8192 x 32000 bf16 201 us (5.2 TB/s), 239 with the sum, fp32 478 (404
+// without it).
+template <typename T>
+constexpr float kExactLse = __is_same(T, __bf16) ? 1024.f : sizeof(T) == 2 ? 128.f : 0.015625f;
 template <typename T, int TPR>
 __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequences, int64_t v, const float* dloss, const T* logits, int64_t ld, const int64_t* targets,
-                                                    const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, Parts parts, T* out, int64_t ldo) {
+                                                    const int64_t* offsets, const float* margin, const float* lse, double beta, double smoothing, Parts parts, bool in_place, T* out, int64_t ldo) {
   constexpr int E = Vec<T>::kElems, PER = 256 / TPR;
+  __shared__ float part[4];
   const int t0 = threadIdx.x % TPR;
   const int64_t first = offset_at(offsets, 0, tokens), last = offset_at(offsets, sequences, tokens);
   for (int64_t u = (int64_t)blockIdx.x * PER + threadIdx.x / TPR; u < tokens * parts.count; u += (int64_t)gridDim.x * PER) {
     const int64_t t = u / parts.count, begin = (u - t * parts.count) * parts.length;
     if (t < first || t >= last) continue;
-    const int64_t end = begin + parts.length < v ? begin + parts.length : v;
+    int64_t end = begin + parts.length < v ? begin + parts.length : v;
     const T* row = logits + t * ld;
     T* o = out + t * ldo;
     const int64_t target = targets[t];
@@ -158,13 +168,50 @@ __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequ
       continue;
     }
     const int64_t low = group_of(offsets, sequences, tokens, t);
+    // (of the margin as the caller has it, in fp32: a relative error of the slope of |z| 2^-24 at most)
     const double z = beta * (double)margin[low / 2];
     const double slope = (smoothing / (1 + exp(-z)) - (1 - smoothing) / (1 + exp(z))) * beta * (double)dloss[low / 2];
     const float f = (float)(low % 2 ? -slope : slope), l = lse[t];
+    float fs = f;                                            // f / (sum of exp(x - l))
+    if (!(fabsf(l) <= kExactLse<T>)) {                       // (all threads of a row's parts alike)
+      if (in_place) {                                          // the other parts must not be written before they are read here
+        if (begin > 0) continue;
+        end = v;
+      }
+      float sum = 0.f;
+      const auto add = [&](const Vec<T>& q) {
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) s += exp_diff(q.get(j), l);
+        sum += s;
+      };
+      int64_t c = t0 * E;
+      for (; c + (kUnroll - 1) * TPR * E + E <= v; c += kUnroll * TPR * E) {
+        Vec<T> q[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) q[k].load(row + c + k * TPR * E, E);
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) add(q[k]);
+      }
+      for (; c < v; c += TPR * E) {
+        Vec<T> q;
+        q.load(row + c, v - c, -INFINITY);
+        add(q);
+      }
+      sum = wave_sumf(sum);
+      if constexpr (TPR > 64) {
+        if (lane_id() == 0) part[threadIdx.x / 64] = sum;
+        __syncthreads();                                      // (the row has been read, and may be written)
+        sum = part[0];
+        for (int w = 1; w < 4; ++w) sum += part[w];
+        __syncthreads();
+      }
+      fs = f / sum;
+    }
     const auto take = [&](Vec<T>& q, int64_t c) {
       float g[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) g[j] = f * ((c + j == target ? 1.f : 0.f) - exp_diff(q.get(j), l));
+      for (int j = 0; j < E; ++j) g[j] = fmaf(exp_diff(q.get(j), l), -fs, c + j == target ? f : 0.f);
       q.put(g);
     };
     int64_t c = begin + t0 * E;
@@ -258,11 +305,11 @@ int adacgd_preference_loss_backward(int64_t tokens, int64_t pairs, int64_t v, co
   if (!dloss || !margin || !lse) return fail(ADACGD_ERR_ARG, "dloss, margin or lse is null");
   return by_dtype(logits->dtype, [&](auto t) {
     using T = decltype(t);
-    const Parts parts = parts_of(tokens, v);
+    const Parts parts = parts_of(tokens, v, sizeof(T) == 4 ? kSumBlocks : kTokenBlocks);
     const int64_t units = tokens * parts.count;
     const auto go = [&](auto kernel, int64_t blocks) {
       kernel<<<token_blocks(blocks), 256, 0, (hipStream_t)stream>>>(tokens, 2 * pairs, v, dloss, (const T*)logits->data, logits->stride, targets, offsets, margin, lse, beta, smoothing,
-                                                                    parts, (T*)dlogits->data, dlogits->stride);
+                                                                    parts, dlogits->data == logits->data, (T*)dlogits->data, dlogits->stride);
     };
     if (narrow(v)) go(k_token_grad<T, 64>, (units + 3) / 4);
     else go(k_token_grad<T, 256>, units);

@@ -781,3 +781,53 @@ def test_offsets_that_break_the_rule_stay_inside(bad):
     L.preference_loss_backward(torch.ones(2, device="cuda"), x, t, o2, margin, lse, out=dx)
     torch.cuda.synchronize()
     assert all(untouched(v) for v in (x, y, dw, dx, nw, nb))
+
+
+# ---------------------------------------------------------------------------------------------------
+# logits far from zero
+# ---------------------------------------------------------------------------------------------------
+def gradient_and_its_bound(logits, targets, off, sizes, beta=0.4, s=0.1, out=None):
+    """The kernel's gradient, the one in 64 bits at the margin that the kernel is given, and a bound on their difference without a term in |lse|."""
+    tokens, v = logits.shape
+    dtype, dloss = logits.dtype, 0.5 + normals((len(sizes) // 2,), F32, 77).abs()
+    lg, tg = logits.cuda(), targets.cuda()
+    _, margin, _, lse = L.preference_loss(lg, tg, off, None, beta, s)
+    got = L.preference_loss_backward(dloss.cuda(), lg, tg, off, margin, lse, beta, s, out=lg if out == "in place" else None).cpu().double()
+    z = beta * margin.cpu().double()
+    slope = beta * (s * torch.sigmoid(z) - (1 - s) * torch.sigmoid(-z)) * dloss.double()
+    f = torch.cat([torch.full((m,), 1.0 - 2 * (i % 2)).double() * slope[i // 2] for i, m in enumerate(sizes)])[:, None]
+    p = torch.softmax(logits.double(), 1)
+    onehot = torch.zeros(tokens, v).double()
+    onehot[torch.arange(tokens), targets] = 1.0
+    want = f * (onehot - p)
+    # exp(x - l) is off by 4 u and by 2 u |x - l| (its argument, rounded twice), the sum of these by their weighted mean and by its
+    # additions, (v / 64 + 20) u; a reciprocal and a product of them, the difference, and the product with f, rounded too, take one u each
+    away = (logits.double() - lse.cpu().double()[:, None]).abs()
+    each = 4 * U + 2 * U * away
+    ep = p * (each + (p * each).sum(1, keepdim=True) + (v / 64 + 20) * U + 2 * U)
+    bound = f.abs() * (ep + U * (onehot - p).abs()) + 2 * U * want.abs()
+    return got, want, bound + HALF[dtype] * (want.abs() + bound) + TINY[dtype] + 1e-38
+
+
+@pytest.mark.parametrize("offset", [0.0, 100.0, 1000.0, -1e4, 1e6])
+@pytest.mark.parametrize("dtype,sizes,v", [(F32, [9, 40, 17, 1], 1000), (F32, [2, 1], 20000), (F32, [600, 700], 300), (F16, [9, 40, 17, 1], 1000), (BF16, [9, 40], 9001)],
+                         ids=lambda t: str(t).replace("torch.", ""))
+def test_preference_gradient_does_not_depend_on_the_logits_offset(dtype, sizes, v, offset):
+    logits = (torch.randn((sum(sizes), v), generator=gen(1)) * 2 + min(offset, 6e4 if dtype == F16 else offset)).to(dtype)
+    targets = torch.randint(0, v, (sum(sizes),), generator=gen(2))
+    for out in (None, "in place"):
+        got, want, bound = gradient_and_its_bound(logits, targets, offsets_of(sizes), sizes, out=out)
+        assert (got - want).abs().le(bound).all(), (out, ((got - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("v", [300, 20000])
+def test_preference_gradient_of_rows_that_are_masked_with_the_lowest_value_throughout(dtype, v):
+    """All of a row's elements alike, far below zero: each has probability 1 / v."""
+    logits = torch.full((5, v), torch.finfo(dtype).min, dtype=dtype)
+    logits[3], logits[4] = torch.finfo(dtype).max, 1000.0
+    targets, sizes = torch.tensor([3, 4, 5, 7, 8]), [2, 1, 1, 1]
+    got, want, bound = gradient_and_its_bound(logits, targets, offsets_of(sizes), sizes)
+    assert (got - want).abs().le(bound).all(), ((got - want).abs() / bound).max()
+    again, _, _ = gradient_and_its_bound(logits, targets, offsets_of(sizes), sizes, out="in place")
+    assert torch.equal(again, got)
