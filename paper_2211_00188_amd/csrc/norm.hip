@@ -188,8 +188,9 @@ __global__ void __launch_bounds__(BLOCK) k_norm_back(const int64_t* offsets, int
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const float g = vy[i].get(j), h = (vx[i].get(j) - m) * r;
-        const float c = g * w[i][j];          // (0 behind the row's end, where g is)
+        // (0 behind the row's end, h too: m r alone may pass the largest number)
+        const float g = vy[i].get(j), h = (i * TPR + t) * E + j < d ? (vx[i].get(j) - m) * r : 0.f;
+        const float c = g * w[i][j];
         a += c;
         q = fmaf(c, h, q);
         sw[i][j] = fmaf(g, h, sw[i][j]);

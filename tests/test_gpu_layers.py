@@ -831,3 +831,19 @@ def test_preference_gradient_of_rows_that_are_masked_with_the_lowest_value_throu
     assert (got - want).abs().le(bound).all(), ((got - want).abs() / bound).max()
     again, _, _ = gradient_and_its_bound(logits, targets, offsets_of(sizes), sizes, out="in place")
     assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [3, 7, 64, 100, 300, 1001, 2056, 5003, 9000, 20001])
+def test_layer_norm_gradients_of_rows_whose_mean_is_large_beside_their_spread(dtype, d):
+    """Equal elements of 1e37, rstd = eps^-1/2: xhat is 0, though mean times rstd passes the largest number.  dx = rstd (c - mean(c))."""
+    rows, rstd = 6, 316.25
+    x = torch.full((rows, d), 1e37).to(dtype)
+    dy, w, mean = normals((rows, d), dtype, 5), 1 + normals((d,), F32, 6, 0.1), x[:, 0].float()
+    dx, dw, db = L.layer_norm_backward(dy.cuda(), x.cuda(), w.cuda(), mean.cuda(), torch.full((rows,), rstd, device="cuda"), offsets_of([4, 2]))
+    c = dy.double() * w.double()
+    want = rstd * (c - c.mean(1, keepdim=True))
+    # a sum of d terms, d / 64 + 24 of them one after the other; each c rounds once, its mean twice more, dx twice
+    bound = rstd * (2 * U * c.abs() + (d / 64 + 28) * U * c.abs().mean(1, keepdim=True)) + 2 * U * want.abs()
+    bound = bound + HALF[dtype] * (want.abs() + bound)
+    assert (dx.cpu().double() - want).abs().le(bound).all() and not dw.any() and torch.isfinite(db).all()
