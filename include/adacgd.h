@@ -377,7 +377,7 @@ typedef struct {
  *   DW       C_g = sum_r A[r] B[r]^T over the rows of g: A [rows x n], B [rows x k], C [groups][n x k]; an empty
  *            group's C_g is zero
  * A and B have one type; C has that type or fp32.  Products are formed on the matrix cores (exactly, from bf16 and
- * fp16) and summed in fp32; one rounding to C's type. */
+ * fp16) and summed in fp32, the parts of a long group's DW in fp64; then they are rounded to C's type. */
 enum adacgd_product { ADACGD_FORWARD = 0, ADACGD_DX = 1, ADACGD_DW = 2 };
 
 /* Device bytes that the call of these sizes needs as workspace (0 for FORWARD and DX). */

@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(K::kThreads) k_group_product(ProductArgs p) {
 
 // Sums of the slices of every group that has several, in their order.  A group that is cut holds a multiple of a slice's rows; it is
 // done by the blocks of the first of these, so that there are as many as slices and not as groups (a thousand groups of which none
-// is cut: 25 us).
+// is cut: 25 us).  In fp64: there may be a thousand slices, of one group.
 template <typename O>
 __global__ void __launch_bounds__(256) k_join(ProductArgs p) {
   const int64_t row = (int64_t)blockIdx.y << p.shift;
@@ -546,18 +546,18 @@ __global__ void __launch_bounds__(256) k_join(ProductArgs p) {
   if (e >= size) return;
   const float* from = p.partial + part_number(first, p.shift) * size + e;
   const int64_t have = size - e;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+  double sum[4] = {0, 0, 0, 0};
+#pragma unroll 8
   for (int64_t j = 0; j < count; ++j) {
     Vec<float> v;
     v.load(from + j * size, have);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sum[q] += v.get(q);
+    for (int q = 0; q < 4; ++q) sum[q] += (double)v.get(q);
   }
   O* c = (O*)p.c + g * p.gsc;
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    if (q < have) c[(e + q) / p.k * p.ldc + (e + q) % p.k] = from_float<O>(sum[q]);
+    if (q < have) c[(e + q) / p.k * p.ldc + (e + q) % p.k] = from_float<O>((float)sum[q]);
 }
 
 // FORWARD with few rows to a group (tokens served one by one): bound by reading the weights once.  A block has 16 rows of a group

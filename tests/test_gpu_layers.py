@@ -847,3 +847,25 @@ def test_layer_norm_gradients_of_rows_whose_mean_is_large_beside_their_spread(dt
     bound = rstd * (2 * U * c.abs() + (d / 64 + 28) * U * c.abs().mean(1, keepdim=True)) + 2 * U * want.abs()
     bound = bound + HALF[dtype] * (want.abs() + bound)
     assert (dx.cpu().double() - want).abs().le(bound).all() and not dw.any() and torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [[262144], [3, 262144, 0, 70]], ids=lambda s: str(len(s)))
+def test_groups_sums_of_many_slices(dtype, sizes):
+    """One row of a long group weighs 2^24, 383 far ones 1 each, which a sum in fp32 that goes from the one to the others would lose."""
+    n = k = 64
+    first = sizes[0] if len(sizes) > 1 else 0
+    x, dy = torch.zeros((sum(sizes), k)), torch.zeros((sum(sizes), n))
+    x[first], dy[first] = 4096.0, 4096.0
+    far = first + 65536 + 512 * torch.arange(383)
+    x[far], dy[far] = 1.0, 1.0
+    dw = L.group_matmul_dw(dy.to(dtype).cuda(), x.to(dtype).cuda(), offsets_of(sizes)).cpu()
+    want = torch.tensor(2 ** 24 + 383, dtype=torch.float64).float()
+    assert (dw[1 if len(sizes) > 1 else 0] == want).all(), (dw.max() - want)
+    # numbers: at most 4096 rows are added up in fp32, each addition a step, 2 u, of a partial sum, before the parts are joined
+    x, dy = torch.randn((sum(sizes), k), generator=gen(1)).to(dtype).cuda(), torch.randn((sum(sizes), n), generator=gen(2)).to(dtype).cuda()
+    dw = L.group_matmul_dw(dy, x, offsets_of(sizes))
+    for g, (a, b) in enumerate(spans(sizes)):
+        xd, dyd = x[a:b].double(), dy[a:b].double()
+        want, size = (dyd.t().contiguous() @ xd), (dyd.abs().t().contiguous() @ xd.abs())
+        assert (dw[g].double() - want).abs().le(2 * U * min(4096, b - a) * size + U * want.abs()).all(), g
