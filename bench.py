@@ -40,11 +40,11 @@ COUNTERS_JSON = os.path.join(ROOT, "profiles", "counters.json")
 CSRC = os.path.join(ROOT, "paper_2211_00188_amd", "csrc")
 
 
-NOT_THE_STEPS = ("engine.hip", "layers.h", "products.hip", "norm.hip", "preference.hip")     # host code; operators of other models
+NOT_THE_STEPS = ("layers.h", "products.hip", "norm.hip", "preference.hip")     # operators of other models
 
 
 def kernel_sources_digest():
-    """sha256 over the sources of the step's kernels: counter figures are only valid for the code they were taken on."""
+    """sha256 over the sources of the step's kernels and of what launches them: counter figures are only valid for the code they were taken on."""
     h = hashlib.sha256()
     for fn in sorted(os.listdir(CSRC)):
         if fn.endswith((".hip", ".h")) and fn not in NOT_THE_STEPS:
