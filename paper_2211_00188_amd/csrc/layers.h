@@ -62,6 +62,14 @@ struct Slice {
   int64_t first, last;  // rows of the whole group
 };
 __host__ __device__ inline int64_t slice_numbers(int64_t rows, int64_t groups, int shift) { return (rows >> shift) + groups; }
+// First number of a group's slices.
+__host__ __device__ inline int64_t first_number(int64_t first_row, int64_t group, int shift) { return (first_row >> shift) + group; }
+
+// Where partial sums are kept for the slices of groups of more than 2^shift rows only: from 2 (first row >> shift) on.  The
+// next such group begins behind the last slice, and the number of places does not depend on the number of groups.
+__host__ __device__ inline int64_t part_number(int64_t first, int shift) { return 2 * (first >> shift); }
+__host__ __device__ inline int64_t part_numbers(int64_t rows, int shift) { return 2 * (rows >> shift) + 1; }
+
 __device__ __forceinline__ int64_t offset_at(const int64_t* offsets, int64_t i, int64_t rows) {
   const int64_t o = offsets[i];
   return o < 0 ? 0 : o > rows ? rows : o;
@@ -84,7 +92,7 @@ __device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t grou
     const int64_t step = (count + 63) / 64;
     const bool here = lane * step < count;
     const int64_t g = low + (here ? lane * step : 0);
-    const uint64_t m = ballot(here && (offset_at(offsets, g * each, rows) >> shift) + g <= number);
+    const uint64_t m = ballot(here && first_number(offset_at(offsets, g * each, rows), g, shift) <= number);
     if (m == 0) return s;
     const int64_t hit = 63 - __builtin_clzll(m);          // (the last of them)
     low += hit * step;
@@ -94,7 +102,7 @@ __device__ __forceinline__ Slice find_slice(const int64_t* offsets, int64_t grou
   s.first = offset_at(offsets, low * each, rows);
   s.last = offset_at(offsets, (low + 1) * each, rows);
   if (s.last < s.first) s.last = s.first;
-  const int64_t j = number - ((s.first >> shift) + low);
+  const int64_t j = number - first_number(s.first, low, shift);
   s.begin = s.first + (j << shift);
   if (s.begin >= s.last && j > 0) return s;
   s.group = low;
@@ -117,8 +125,6 @@ __device__ __forceinline__ int64_t group_of(const int64_t* offsets, int64_t grou
   return low;
 }
 
-// First number of a group's slices.
-__device__ __forceinline__ int64_t first_number(int64_t first_row, int64_t group, int shift) { return (first_row >> shift) + group; }
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_or0f(float v) { return __uint_as_float(dpp_or0<CTRL, ROWS>(__float_as_uint(v))); }

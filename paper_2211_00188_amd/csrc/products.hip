@@ -76,11 +76,6 @@ struct ProductArgs {
   int n, k, shift;
 };
 
-// Where the sums of a cut group's slices lie: from 2 (first row >> shift) on.  Only groups of more than 2^shift rows are cut, so that the
-// next of them begins behind the last slice, and the number of places does not depend on the number of groups.
-__host__ __device__ inline int64_t part_number(int64_t first, int shift) { return 2 * (first >> shift); }
-inline int64_t part_numbers(int64_t rows, int shift) { return 2 * (rows >> shift) + 1; }
-
 // The block's tile among those of slices that exist, of at most 64 groups.
 __device__ __forceinline__ bool find_tile(const ProductArgs& p, Slice& s, int64_t& j) {
   const int lane = (int)lane_id();

@@ -167,3 +167,58 @@ def test_the_preference_workloads_parts_are_views_in_order():
     assert wl.worker_rows()[-1] == len(wl.targets) == len(wl.features) == len(wl.ref) and wl.worker_rows()[0] == 0
     again = W.preference(n=3, pairs=7, width=8, vocab=11, length=6)
     assert np.array_equal(again.features, wl.features) and np.array_equal(again.targets, wl.targets)
+
+
+@pytest.fixture(scope="module")
+def helpers(tmp_path_factory):
+    """The host side of csrc/layers.h's numbering of slices, as it is compiled."""
+    import shutil
+    import subprocess
+    from paper_2211_00188_amd import build as B
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not shutil.which(hipcc):
+        pytest.skip("no hipcc")
+    where = tmp_path_factory.mktemp("helpers")
+    names = {"slice_numbers": 3, "first_number": 3, "part_number": 2, "part_numbers": 2}
+    with open(where / "helpers.hip", "w") as f:
+        f.write('#include "%s/layers.h"\n' % B.CSRC)
+        for name, count in names.items():
+            longs = ["int64_t a", "int64_t b"][:count - 1]
+            f.write('extern "C" int64_t t_%s(%s, int shift) { return adacgd::%s(%s, shift); }\n'
+                    % (name, ", ".join(longs), name, ", ".join(v[-1] for v in longs)))
+    subprocess.run([hipcc, "--cuda-host-only", "-std=c++17", "-fPIC", "-shared", "-o", str(where / "helpers.so"), str(where / "helpers.hip")],
+                   check=True, capture_output=True)
+    lib = C.CDLL(str(where / "helpers.so"))
+    for name, count in names.items():
+        f = getattr(lib, "t_" + name)
+        f.argtypes, f.restype = [C.c_int64] * (count - 1) + [C.c_int], C.c_int64
+    return lib
+
+
+@pytest.mark.parametrize("shift", [2, 4, 6, 7, 8, 13])
+def test_the_librarys_numbers_of_slices_are_within_its_launches_and_workspaces(helpers, shift):
+    """Every slice of every group has a number of its own below what is launched, and every slice of a cut group a place of its own
+    inside the workspace, to the last row."""
+    rng = np.random.default_rng(100 + shift)
+    for trial in range(300):
+        groups = int(rng.integers(1, 40))
+        sizes = (rng.integers(0, 5 << shift, groups) * (rng.random(groups) < 0.75)).astype(int)
+        sizes[rng.random(groups) < 0.2] = (1 << shift) + int(rng.integers(-1, 2))
+        o = int(rng.integers(0, 3 << shift)) + np.concatenate([[0], np.cumsum(sizes)])
+        rows = int(o[-1]) + int(rng.integers(0, 3)) * int(rng.integers(0, 2 << shift))
+        count = [max(1, -(-int(m) >> shift)) for m in sizes]
+        numbers = [helpers.t_first_number(int(o[g]), g, shift) + j for g in range(groups) for j in range(count[g])]
+        assert numbers[0] >= 0 and all(a < b for a, b in zip(numbers, numbers[1:])) and numbers[-1] < helpers.t_slice_numbers(rows, groups, shift)
+        places = [helpers.t_part_number(int(o[g]), shift) + j for g in range(groups) if sizes[g] > 1 << shift for j in range(count[g])]
+        assert len(set(places)) == len(places) and max(places, default=0) < helpers.t_part_numbers(rows, shift) and min(places, default=0) >= 0
+
+
+@pytest.mark.parametrize("sizes,n,k", [([65536], 512, 512), ([262144], 64, 64), ([30000] + [2] * 300, 256, 256), ([16384], 1032, 1040)])
+def test_workspace_of_cut_groups_holds_two_slices_of_the_longest(sizes, n, k):
+    """A group that is cut has two slices at least, and their partial sums are fp32 matrices side by side."""
+    lib, size = L._library(), C.c_int64(-1)
+    for dtype in (0, 1, 2):
+        assert lib.adacgd_group_matmul_workspace_bytes(2, dtype, sum(sizes), len(sizes), n, k, C.byref(size)) == 0
+        assert size.value >= 2 * n * k * 4 and size.value % 256 == 0
+    assert lib.adacgd_layer_norm_backward_workspace_bytes(sum(sizes), len(sizes), n, C.byref(size)) == 0
+    assert size.value >= 2 * 2 * n * 4
