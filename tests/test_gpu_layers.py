@@ -869,3 +869,58 @@ def test_groups_sums_of_many_slices(dtype, sizes):
         xd, dyd = x[a:b].double(), dy[a:b].double()
         want, size = (dyd.t().contiguous() @ xd), (dyd.abs().t().contiguous() @ xd.abs())
         assert (dw[g].double() - want).abs().le(2 * U * min(4096, b - a) * size + U * want.abs()).all(), g
+
+
+# ---------------------------------------------------------------------------------------------------
+# more rows than one launch has blocks: each row as in a call that has it in its first turn
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,d,dtype", [(70001, 64, F32), (40001, 100, BF16), (20003, 500, F16), (9001, 1000, BF16), (4999, 1501, F32), (5001, 4000, BF16), (4100, 5003, F16),
+                                          (4099, 8192, F32), (4100, 9000, BF16), (2500, 9000, F32), (2100, 20001, BF16)])
+def test_layer_norm_of_many_rows_is_that_of_few(rows, d, dtype):
+    x = torch.randn((rows, d), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(dtype)
+    w, b = 1 + normals((d,), F32, 1, 0.1).cuda(), normals((d,), F32, 2, 0.1).cuda()
+    y, mean, rstd = L.layer_norm(x, w, b)
+    dx, dw, db = L.layer_norm_backward(x, x, w, mean, rstd)
+    for a in range(0, rows, 1999):
+        part = slice(a, a + 1999)
+        py, pm, pr = L.layer_norm(x[part], w, b)
+        assert torch.equal(y[part], py) and torch.equal(mean[part], pm) and torch.equal(rstd[part], pr)
+        assert torch.equal(dx[part], L.layer_norm_backward(x[part], x[part], w, pm, pr)[0])
+    # dbias: the rows of a slice, 1/1024 of all or a few, are added up in fp32, the slices in fp64
+    size = x.double().abs().sum(0)
+    assert (db[0].double() - x.double().sum(0)).abs().le((rows / 1024 + 20) * 2 * U * size).all()
+    same, _, _ = L.layer_norm(x, w, b, out=x)
+    assert torch.equal(same, y)
+
+
+@pytest.mark.parametrize("rows,d,pad", [(17001, 1003, 0), (70001, 24, 3), (33000, 9, 1), (3, 6000001, 5)])      # (rows without gaps are one row)
+def test_dropout_of_many_elements_is_that_of_few(rows, d, pad):
+    x = gpu(torch.randn((rows, d), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(BF16), pad)
+    whole = L.dropout(x, 0.2, 9, step=5, residual=x, out=gpu(x, pad))
+    if rows > 100:
+        parts = [L.dropout(x[a:a + 7000], 0.2, 9, step=5, residual=x[a:a + 7000], first=a * d) for a in range(0, rows, 7000)]
+        assert torch.equal(torch.cat(parts), whole)
+    else:
+        step = 4000000
+        for r in range(rows):
+            for a in range(0, d, step):
+                piece = x[r:r + 1, a:a + step]
+                assert torch.equal(L.dropout(piece, 0.2, 9, step=5, residual=piece, first=r * d + a), whole[r:r + 1, a:a + step])
+    assert untouched(whole)
+
+
+def test_preference_loss_of_many_tokens_is_that_of_few():
+    tokens, v = 4500000, 9
+    x = torch.randn((tokens, v), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    t = torch.randint(-1, v, (tokens,), generator=torch.Generator("cuda").manual_seed(2), device="cuda")
+    off = torch.arange(0, tokens + 1, 3, device="cuda")[:2 * (tokens // 6) + 1]
+    loss, margin, logp, lse = L.preference_loss(x, t, off, None, 0.3)
+    one = torch.ones(len(loss), device="cuda")
+    grad = L.preference_loss_backward(one, x, t, off, margin, lse, 0.3)
+    for a in (0, 2100000, tokens - 1200000):                       # (token rows; multiples of 6, 1200000 of them each)
+        rows, pairs = slice(a, a + 1200000), slice(a // 6, a // 6 + 200000)
+        o = off[:400001]
+        part = L.preference_loss(x[rows], t[rows], o, None, 0.3)
+        assert all(torch.equal(p, w) for p, w in zip(part, (loss[pairs], margin[pairs], logp[rows], lse[rows])))
+        assert torch.equal(L.preference_loss_backward(one[pairs], x[rows], t[rows], o, part[1], part[3], 0.3), grad[rows])
+    assert torch.equal(L.preference_loss_backward(one, x, t, off, margin, lse, 0.3, out=x), grad)
