@@ -389,7 +389,8 @@ int adacgd_group_matmul(int32_t product, int64_t rows, int64_t groups, int64_t n
 
 /* Layer normalisation of the rows of x [rows x d]: y = (x - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps),
  * var the mean square of x - mean.  weight, bias: fp32 [d] or NULL (1 and 0).  mean, rstd: fp32 [rows], written; both
- * NULL if no backward pass follows.  y has the type of x and may be x. */
+ * NULL if no backward pass follows.  y has the type of x and may be x.  eps must be 0 or a number of fp32.  Rows whose sum, or sum of
+ * squares around the mean, passes fp32's largest number come out as such sums make them. */
 int adacgd_layer_norm(int64_t rows, int64_t d, const adacgd_tensor* x, const float* weight, const float* bias, double eps,
                       const adacgd_tensor* y, float* mean, float* rstd, void* stream);
 

@@ -416,7 +416,8 @@ int adacgd_layer_norm(int64_t rows, int64_t d, const adacgd_tensor* x, const flo
   ADACGD_TRY(check_tensor(x, "x", rows, d, false, false));
   ADACGD_TRY(check_tensor(y, "y", rows, d, false, false));
   if (x->dtype != y->dtype) return fail(ADACGD_ERR_ARG, "x and y differ in type");
-  if (!std::isfinite(eps) || eps < 0) return fail(ADACGD_ERR_ARG, "eps must be finite and >= 0");
+  // (it is added to var in fp32: what that type has no number for would act as another one)
+  if (!std::isfinite((float)eps) || eps < 0 || (eps > 0 && (float)eps == 0.f)) return fail(ADACGD_ERR_ARG, "eps must be finite and >= 0 in fp32");
   if (!mean != !rstd) return fail(ADACGD_ERR_ARG, "mean and rstd are given together or not at all");
   if (rows == 0) return ADACGD_OK;
   return by_dtype(x->dtype, [&](auto t) {

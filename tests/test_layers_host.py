@@ -222,3 +222,8 @@ def test_workspace_of_cut_groups_holds_two_slices_of_the_longest(sizes, n, k):
         assert size.value >= 2 * n * k * 4 and size.value % 256 == 0
     assert lib.adacgd_layer_norm_backward_workspace_bytes(sum(sizes), len(sizes), n, C.byref(size)) == 0
     assert size.value >= 2 * 2 * n * 4
+
+
+@pytest.mark.parametrize("eps", [1e-46, 5e-324, 1e39])
+def test_norms_refuse_an_eps_that_fp32_has_no_number_for(eps):
+    refused("adacgd_layer_norm", list(dict(NORM, eps=eps).values()), ARG, "eps")
