@@ -501,7 +501,7 @@ int adacgd_dropout(int64_t rows, int64_t d, const adacgd_tensor* x, const adacgd
   if (!(p >= 0 && p <= 1)) return fail(ADACGD_ERR_ARG, "p must be in [0, 1]");
   if (layer == 0xffffffffu) return fail(ADACGD_ERR_ARG, "layer must be below 2^32 - 1");
   if (rows == 0) return ADACGD_OK;
-  if (first + (uint64_t)(rows * d) < first) return fail(ADACGD_ERR_ARG, "first and the elements pass 2^64");
+  if (first + (uint64_t)(rows * d - 1) < first) return fail(ADACGD_ERR_ARG, "first and the elements pass 2^64");
   const uint32_t cut = (uint32_t)std::floor(p * 65536 + 0.5);
   const float scale = cut == 65536 ? 0.f : (float)(65536.0 / (65536 - cut));
   if (rows > 1 && x->stride == d && out->stride == d && (!residual || residual->stride == d)) { d *= rows; rows = 1; }

@@ -924,3 +924,11 @@ def test_preference_loss_of_many_tokens_is_that_of_few():
         assert all(torch.equal(p, w) for p, w in zip(part, (loss[pairs], margin[pairs], logp[rows], lse[rows])))
         assert torch.equal(L.preference_loss_backward(one[pairs], x[rows], t[rows], o, part[1], part[3], 0.3), grad[rows])
     assert torch.equal(L.preference_loss_backward(one, x, t, off, margin, lse, 0.3, out=x), grad)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_dropout_of_the_last_elements_that_64_bits_number(dtype):
+    x, first = normals((3, 24), dtype, 1), (1 << 64) - 72
+    assert torch.equal(L.dropout(x.cuda(), 0.3, 5, first=first).cpu(), dropped(x, None, 0.3, 5, first=first))
+    with pytest.raises(E.AdaCGDError, match="2\\^64"):
+        L.dropout(x.cuda(), 0.3, 5, first=first + 1)
