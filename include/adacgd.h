@@ -420,7 +420,8 @@ int adacgd_dropout(int64_t rows, int64_t d, const adacgd_tensor* x, const adacgd
  *   loss[p] = (1 - smoothing) log(1 + exp(-beta margin[p])) + smoothing log(1 + exp(beta margin[p])).
  * Tokens whose target is outside [0, v) (prompts, padding) do not count: logp is 0 there and neither logits nor ref
  * matter.  ref: fp32 [tokens], NULL for zeros.  loss, margin: fp32 [pairs]; logp and lse (log of the sum of
- * exponentials, 0 at tokens that do not count): fp32 [tokens], all written.  Sums over tokens are held in fp64. */
+ * exponentials, 0 at tokens that do not count): fp32 [tokens], all written.  Sums over tokens are held in fp64.  A row with an element
+ * of +inf, or with nothing but -inf, has no softmax: lse of the one and logp of both are NaN. */
 int adacgd_preference_loss_workspace_bytes(int64_t tokens, int64_t pairs, int64_t v, int64_t* bytes);
 int adacgd_preference_loss(int64_t tokens, int64_t pairs, int64_t v, const adacgd_tensor* logits, const int64_t* targets,
                            const int64_t* offsets, const float* ref, double beta, double smoothing, float* loss,
@@ -428,8 +429,9 @@ int adacgd_preference_loss(int64_t tokens, int64_t pairs, int64_t v, const adacg
 
 /* dlogits = sum_p dloss[p] d loss[p] / d logits, zero at tokens that do not count; dloss: fp32 [pairs].  dlogits has the
  * type of logits and may be logits.  The slope of the loss is that at margin as it is given, in fp32: a relative error of up to
- * 2^-24 |beta margin|.  What rounding lse to fp32 took from it does not enter: where that could be seen in dlogits' type, the rows'
- * sums are formed again around lse. */
+ * 2^-24 |beta margin| of each of its two terms.  What rounding lse to fp32 took from it does not enter: where that could be seen in dlogits' type, the rows'
+ * sums are formed again around lse.  In fp16 most elements of a large vocabulary's rows lie below the type's smallest number unless
+ * dloss carries a scale. */
 int adacgd_preference_loss_backward(int64_t tokens, int64_t pairs, int64_t v, const float* dloss, const adacgd_tensor* logits,
                                     const int64_t* targets, const int64_t* offsets, const float* margin, const float* lse,
                                     double beta, double smoothing, const adacgd_tensor* dlogits, void* stream);

@@ -11,10 +11,10 @@ namespace {
 // A row is held in registers: `TPR` threads, `NV` vectors of 16 bytes each, vector i of thread t being number i TPR + t of the
 // row, so that x is read once whatever is made of it.  One wavefront to a row needs no barrier; rows past what 1024 threads
 // hold are read again (they are in cache).  The least threads that hold the row are taken, with one or two vectors each: four need
-// the registers that rows on their way ahead take (65536 x 2048 bf16 forward: 168 us by a wavefront to a row, 119 by 256 threads).  Short
-// rows share a wavefront: 10^6 of 64 elements 71 us forward (289 by a wavefront each), 3 10^5 of 256 elements 65 us forward and 110
-// backward (87 and 215).  Bound by memory: a pass over x and one over y, or over dy, x and dx; 65536 x 2048 bf16 119 us forward
-// (4.5 TB/s) and 199 backward (4.0), fp32 213 and 330 (5.0 and 4.9).
+// the registers that rows on their way ahead take (65536 x 2048 bf16 forward: 168 us by a wavefront to a row, 116 by 256 threads).  Short
+// rows share a wavefront: 10^6 of 64 elements 66 us forward (289 by a wavefront each), 3 10^5 of 256 elements 62 us forward and 109
+// backward (87 and 215).  Bound by memory: a pass over x and one over y, or over dy, x and dx; 65536 x 2048 bf16 116 us forward
+// (4.6 TB/s) and 190 backward (4.2), fp32 213 and 327 (5.0 and 4.9).
 template <int TPR, int BLOCK>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
   if constexpr (TPR == 16) return row16_sumf(v);
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(BLOCK) k_norm(const T* x, int64_t ldx, const f
   }
 }
 
-// Rows longer than registers hold.
+// Rows longer than registers hold, in three passes over the row: 16384 x 12288 fp32 643 us forward (2.5 TB/s of x and y once).
 template <typename T>
 __global__ void __launch_bounds__(1024) k_norm_long(const T* x, int64_t ldx, const float* weight, const float* bias, int64_t rows, int d, float eps,
                                                     T* y, int64_t ldy, float* mean, float* rstd) {
@@ -242,7 +242,8 @@ __global__ void __launch_bounds__(BLOCK) k_norm_back(const int64_t* offsets, int
   finish(sb, ob);
 }
 
-// Rows longer than registers hold: dx row by row, and the sums by blocks of 256 columns of a slice.
+// Rows longer than registers hold: dx row by row, and the sums by blocks of 256 columns of a slice.  16384 x 12288 fp32 993 us (2.4 TB/s
+// of dy, x and dx once).
 template <typename T>
 __global__ void __launch_bounds__(1024) k_norm_long_dx(const int64_t* offsets, int64_t groups, int64_t rows, const T* dy, int64_t ldy, const T* x, int64_t ldx,
                                                        const float* weight, const float* mean, const float* rstd, int d, T* dx, int64_t ldd) {

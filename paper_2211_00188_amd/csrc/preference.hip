@@ -45,8 +45,8 @@ inline bool narrow(int64_t v) { return v <= 8192; }      // a wavefront to a row
 
 // Largest element and sum of exponentials of (a part of) every row that counts, in one pass: a thread's sum is scaled down
 // when one of its vectors has a larger element.  The target's logit is put aside by the part that has it.  Bound by memory where
-// a row is long: 8192 x 32000 bf16 110 us (4.8 TB/s; in two passes over a row 479), 32768 x 4096 by a wavefront each 54 (by 256
-// threads 104); 10^5 rows of 250 wait for the chain of target, row and sum: 75 us, 0.7 TB/s.
+// a row is long: 8192 x 32000 bf16 110 to 116 us (4.5 to 4.8 TB/s; in two passes over a row 479), 32768 x 4096 by a wavefront each 54 (by 256
+// threads 104); 10^5 rows of 250 wait for the chain of target, row and sum: 72 us, 0.7 TB/s.
 template <typename T, int TPR>
 __global__ void __launch_bounds__(256) k_token(int64_t tokens, int64_t sequences, int64_t v, const T* logits, int64_t ld, const int64_t* targets, const int64_t* offsets,
                                                Parts parts, Lse* out, float* at_target) {
@@ -103,7 +103,8 @@ __global__ void __launch_bounds__(256) k_token(int64_t tokens, int64_t sequences
   }
 }
 
-// Log-probabilities of a pair's tokens, the sums of their differences from the reference, and the loss.
+// Log-probabilities of a pair's tokens, the sums of their differences from the reference, and the loss.  Bound by the longest pair, which is
+// one block's: with k_token, 32768 tokens of 250 logits in one pair take 78 us, in sixteen 27.
 constexpr int kPairThreads = 512;
 __global__ void __launch_bounds__(kPairThreads) k_pair(int64_t tokens, int64_t v, const int64_t* targets, const int64_t* offsets, int64_t parts, const Lse* in, const float* at_target,
                                                        const float* ref, double beta, double smoothing, float* loss, float* margin, float* logp, float* lse) {
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(256) k_token_grad(int64_t tokens, int64_t sequ
       continue;
     }
     const int64_t low = group_of(offsets, sequences, tokens, t);
-    // (of the margin as the caller has it, in fp32: a relative error of the slope of |z| 2^-24 at most)
+    // (of the margin as the caller has it, in fp32: a relative error of |z| 2^-24 at most in either term of the slope)
     const double z = beta * (double)margin[low / 2];
     const double slope = (smoothing / (1 + exp(-z)) - (1 - smoothing) / (1 + exp(z))) * beta * (double)dloss[low / 2];
     const float f = (float)(low % 2 ? -slope : slope), l = lse[t];

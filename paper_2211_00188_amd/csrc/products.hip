@@ -61,7 +61,8 @@ __device__ __forceinline__ bool tile_of(uint32_t block, const Patches& p, int64_
 }
 
 // Where one load of a wavefront shows all groups, the slices that exist are counted instead: every die gets an eighth of the
-// tiles, down bands of four slices.  (16 groups of 1024 rows, 2048 columns: 20 patches for 8 dies took 305 us, this takes 225.)
+// tiles, down bands of four slices.  (16 groups of 1024 rows, 2048 columns: 20 patches for 8 dies took 305 us, this takes 225 to
+// 237; as ragged as shards are, 72 slices for 64 slices' worth of rows, 309.)
 constexpr int kCounted = 64;
 
 struct ProductArgs {
